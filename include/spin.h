@@ -5,8 +5,11 @@
  * products, and fixed-point truncation (spin_share, spin_open,
  * spin_beaver_matmul, spin_beaver_mul, spin_trunc).  Further down: the same
  * over Z_2^32 and Z_2^128 (spin32_*, spin128_*), binary shares (spin_b*),
- * and a public linear combination with fused truncation.  Measurement aids
- * (per-kernel event timing, an MFMA rate probe) are declared in spin_bench.h.
+ * a public linear combination with fused truncation, and for generating token by
+ * token a paged cache of shared keys and values, the attention products of a tree
+ * of drafted tokens over it and a relative position bias (spin_cache_*,
+ * spin_relbias_*).  Measurement aids (per-kernel event timing, an MFMA rate
+ * probe) are declared in spin_bench.h.
  *
  * Conventions that hold for every entry point
  * -------------------------------------------
@@ -310,6 +313,118 @@ spin_status spin32_trunc(int n, size_t count, int f, const uint32_t *x,
                          const uint32_t *r, const uint32_t *r_top, const uint32_t *r_msb,
                          uint32_t *out, spin_stream stream);
 spin_status spin_cast_64_to_32(const uint64_t *in, size_t count, uint32_t *out, spin_stream stream);
+
+/* ---- A paged cache of shared keys and values, and what reads it --------------------------------------
+ * Generating token by token multiplies the same K and V again in every step.  A row of K or V is therefore
+ * opened once, against a mask b dealt for it, and kept: F = sum_i (x_i - b_i) is public, and every later product
+ * with that row needs only its own fresh mask of the other factor (Section 4.3's update with F fixed).
+ * A cached row takes n + 1 words an element: slot 0 holds F, slot 1 holds b_0 + F (which folds party 0's public term E.F
+ * into its product) and slot 1 + i holds b_i.  Slots 1 to n are themselves a sharing of the row.
+ *
+ * Rows live in pages of page_tokens positions; table[b][j] is the page that holds positions j * page_tokens and on of
+ * sequence b.  Sequences may share pages (a fork) as long as none of them writes there.  table, contexts, counts and page lists are
+ * DEVICE arrays of int32_t (4-byte aligned); what is wrong in them cannot be refused by the call and never makes a kernel
+ * leave the buffers: an entry outside [0, pages) is a page that is not there, whose rows are not written and not visible, and
+ * neither are positions past the end of the table.  Entry points spin32_* take the same structure with pools of uint32_t.        */
+typedef struct {
+    int n;                 /* parties                                                                            */
+    int pages;             /* pages of each pool                                                                 */
+    int heads;             /* cached heads                                                                       */
+    int page_tokens;       /* positions a page: a power of two, 16 to 4096                                       */
+    int dim;               /* elements of a head's row: a multiple of 8, 8 to 256                                */
+    void *K, *V;           /* pools, each [n + 1][pages][heads][page_tokens][dim] ring elements                  */
+    int batch;             /* sequences                                                                          */
+    int table_pages;       /* entries of a sequence in the table                                                 */
+    const int32_t *table;  /* [batch][table_pages]                                                               */
+} spin_cache;
+
+/* A learned relative position bias: one shared word a head and bucket, added to scores of precision f after truncation.
+ * bucket_of[d + reach] is the bucket of distance d = key position - query position, distances beyond reach count as reach;
+ * entries outside [0, buckets) add nothing.                                                                                  */
+typedef struct {
+    int buckets;               /* 1 to 1024                                                                      */
+    int reach;                 /* 0 to 65535                                                                     */
+    const int32_t *bucket_of;  /* device, [2 * reach + 1]                                                        */
+    const void *table;         /* device, shares [n][heads][buckets] of ring elements                            */
+} spin_relbias;
+
+/* Opens new rows of keys and values and writes them into their pages: row s < count[b] of sequence b goes to position
+ * start[b] + s.  Kx, Vx: shares, Kb, Vb: their masks, all [n][batch][heads][rows][dim].  count: [batch], or NULL for `rows` each.
+ * Rows whose page is not there, or whose position is negative, are left out.                                              */
+spin_status spin_cache_append(const spin_cache *c, int rows, const int32_t *start, const int32_t *count,
+                              const uint64_t *Kx, const uint64_t *Kb, const uint64_t *Vx, const uint64_t *Vb, spin_stream stream);
+
+/* Copies whole pages of both pools, src[p] to dst[p] for p < pairs (a fork about to be written, a pool being compacted).  The
+ * table is not looked at.  Pairs with a page that is not there are left out; no page may be written twice, or read and written, in one call.  */
+spin_status spin_cache_copy(const spin_cache *c, int pairs, const int32_t *src, const int32_t *dst, spin_stream stream);
+
+/* Keeps the accepted ones of `nodes` drafted tokens: the row at position context[b] + kept[b][j] moves to context[b] + j, for
+ * j < kept_count[b], in both pools.  kept: [batch][nodes], strictly ascending in every sequence.  Nothing moves where
+ * context[b] < 0; indices outside [0, nodes) are left out.  1 <= nodes <= 64.                                                              */
+#define SPIN_MAX_NODES 64
+spin_status spin_cache_compact(const spin_cache *c, int nodes, const int32_t *context, const int32_t *kept,
+                               const int32_t *kept_count, spin_stream stream);
+
+/* Scores of `nodes` new tokens a sequence over the cache.  The tokens, a single one or a tree of drafted ones, stand
+ * in the cache at positions context[b] .. context[b] + nodes - 1; node m sees all positions below context[b], and drafted node j where
+ * bit j of tree[b][m] is set (tree NULL: the nodes up to itself).  A sequence with context[b] < 0 sees nothing.  For every
+ * query head h (cached head h / (heads / c->heads)) and node m, with E = sum_i (Q_i - A_i), at every visible position t < columns:
+ *     Z_i = C_i + E . slot(1 + i)[t] + A_i . slot(0)[t],     out = f > 0 ? Truncate(Z, f) : Z,     out_i += bias_i[h][bucket]
+ * and everywhere else the public constant `masked` (party 0 holds it, the others 0).
+ * Q, A: [n][batch][heads][nodes][dim]; C, r, r_top, r_msb, out: [n][batch][heads][nodes][columns].  Triples satisfy sum_i C_i = (sum A_i)(sum b_i)
+ * with the masks that the rows were opened with.  tuple pointers are ignored when f = 0; out may alias C, and r, r_top or r_msb.
+ * bias may be NULL; with it depth ([batch][nodes] or NULL: 0, 1, ..) is the distance of a node behind the context: its position is
+ * context[b] + depth[b][m] as query and as key.  heads is a multiple of c->heads; c->V is not looked at.  0 <= f <= 61.          */
+spin_status spin_cache_scores(const spin_cache *c, int heads, int nodes, int columns, int f, const int32_t *context,
+                              const uint64_t *tree, const uint64_t *Q, const uint64_t *A, const uint64_t *C,
+                              const uint64_t *r, const uint64_t *r_top, const uint64_t *r_msb, uint64_t masked,
+                              const spin_relbias *bias, const int32_t *depth, uint64_t *out, spin_stream stream);
+
+/* The weighted sums of cached values: with E = sum_i (P_i - A_i), over the positions t < columns that node m sees (as above),
+ *     Z_i = C_i + sum_t E[t] slot(1 + i)[t] + A_i[t] slot(0)[t],     out = f > 0 ? Truncate(Z, f) : Z.
+ * P and A count as zero where nothing is seen, whatever they hold there; a node that sees nothing gives Z = C.
+ * P, A: [n][batch][heads][nodes][columns]; C, r, r_top, r_msb, out: [n][batch][heads][nodes][dim].  c->K is not looked at.
+ * workspace: device scratch of spin_cache_values_workspace_bytes() bytes (0 if the arguments are invalid), 256-byte aligned.   */
+spin_status spin_cache_values(const spin_cache *c, int heads, int nodes, int columns, int f, const int32_t *context,
+                              const uint64_t *tree, const uint64_t *P, const uint64_t *A, const uint64_t *C,
+                              const uint64_t *r, const uint64_t *r_top, const uint64_t *r_msb, uint64_t *out,
+                              void *workspace, size_t workspace_bytes, spin_stream stream);
+size_t spin_cache_values_workspace_bytes(const spin_cache *c, int heads, int nodes, int columns);
+
+/* Whole matrices of scores: truncation, relative position bias and mask in one pass.  For x [n][batch][heads][Q][K],
+ *     out = f > 0 ? Truncate(x, f) : x,     out_i += bias_i[h][bucket of k - (q + first)]
+ * where k < lengths[b] (lengths NULL: everywhere) and, if causal != 0, k <= q + first; elsewhere the public constant `masked`.
+ * out may alias any input but the bias.  0 <= f <= 61.                                                                       */
+spin_status spin_relbias_trunc(int n, int batch, int heads, int Q, int K, int first, int causal, const int32_t *lengths, int f,
+                               const uint64_t *x, const uint64_t *r, const uint64_t *r_top, const uint64_t *r_msb,
+                               uint64_t masked, const spin_relbias *bias, uint64_t *out, spin_stream stream);
+
+/* The gradient of that bias: grad_i[h][b] = sum of dS_i[..][h][q][k] over the batch and the positions that are there (as above) and have
+ * bucket b.  dS: [n][batch][heads][Q][K]; grad: [n][heads][buckets], overwritten.  bias->table is not looked at.  (The gradient with
+ * respect to x is dS where the position is there.)                                                                            */
+spin_status spin_relbias_grad(int n, int batch, int heads, int Q, int K, int first, int causal, const int32_t *lengths,
+                              const uint64_t *dS, const spin_relbias *bias, uint64_t *grad, spin_stream stream);
+
+/* The same over Z_2^32 (pools and tables of uint32_t; f <= 29).                                                               */
+spin_status spin32_cache_append(const spin_cache *c, int rows, const int32_t *start, const int32_t *count,
+                                const uint32_t *Kx, const uint32_t *Kb, const uint32_t *Vx, const uint32_t *Vb, spin_stream stream);
+spin_status spin32_cache_copy(const spin_cache *c, int pairs, const int32_t *src, const int32_t *dst, spin_stream stream);
+spin_status spin32_cache_compact(const spin_cache *c, int nodes, const int32_t *context, const int32_t *kept,
+                                 const int32_t *kept_count, spin_stream stream);
+spin_status spin32_cache_scores(const spin_cache *c, int heads, int nodes, int columns, int f, const int32_t *context,
+                                const uint64_t *tree, const uint32_t *Q, const uint32_t *A, const uint32_t *C,
+                                const uint32_t *r, const uint32_t *r_top, const uint32_t *r_msb, uint32_t masked,
+                                const spin_relbias *bias, const int32_t *depth, uint32_t *out, spin_stream stream);
+spin_status spin32_cache_values(const spin_cache *c, int heads, int nodes, int columns, int f, const int32_t *context,
+                                const uint64_t *tree, const uint32_t *P, const uint32_t *A, const uint32_t *C,
+                                const uint32_t *r, const uint32_t *r_top, const uint32_t *r_msb, uint32_t *out,
+                                void *workspace, size_t workspace_bytes, spin_stream stream);
+size_t spin32_cache_values_workspace_bytes(const spin_cache *c, int heads, int nodes, int columns);
+spin_status spin32_relbias_trunc(int n, int batch, int heads, int Q, int K, int first, int causal, const int32_t *lengths, int f,
+                                 const uint32_t *x, const uint32_t *r, const uint32_t *r_top, const uint32_t *r_msb,
+                                 uint32_t masked, const spin_relbias *bias, uint32_t *out, spin_stream stream);
+spin_status spin32_relbias_grad(int n, int batch, int heads, int Q, int K, int first, int causal, const int32_t *lengths,
+                                const uint32_t *dS, const spin_relbias *bias, uint32_t *grad, spin_stream stream);
 
 /* Static description of a status code. */
 const char *spin_status_string(int status);

@@ -42,7 +42,10 @@ typedef enum {
     SPIN_KERNEL_GEMM_RESIDUE = 13,   /* residue GEMM; its packs count as SPIN_KERNEL_PACK */
     SPIN_KERNEL_COMBINE = 14,        /* residues back to ring words */
     SPIN_KERNEL_GEMM_DIRECT = 15,    /* small matmuls in one launch */
-    SPIN_KERNEL_COUNT = 16
+    SPIN_KERNEL_CACHE = 16,          /* spin_cache_append, _copy, _compact */
+    SPIN_KERNEL_ATTENTION = 17,      /* spin_cache_scores, _values */
+    SPIN_KERNEL_RELBIAS = 18,        /* spin_relbias_trunc, _grad */
+    SPIN_KERNEL_COUNT = 19
 } spin_kernel;
 void spin_profile_enable(int on);
 spin_status spin_profile_read(int kernel, double *total_ms, unsigned *launches);

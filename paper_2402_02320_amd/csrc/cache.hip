@@ -1,0 +1,137 @@
+// Upkeep of the paged cache of shares (spin_cache_append, _copy, _compact): pure HBM streams, 16 bytes a lane.
+#include "generation.hpp"
+
+namespace spin {
+namespace {
+
+constexpr int kBlock = 256;
+
+template <class T> struct alignas(16) Vec { T e[16 / sizeof(T)]; };
+
+// One thread: 16 bytes of one new row, all slots.  F = sum (x_i - b_i) stays in registers; a row moves 2n words an element in and n + 1
+// out, each once.  blockIdx.y = sequence and head, blockIdx.z = K or V.
+template <int NP, class T> __global__ __launch_bounds__(kBlock) void append_kernel(AppendArgs<T> a)
+{
+    constexpr int VEC = 16 / sizeof(T);
+    const unsigned per_row = a.c.dim / VEC;
+    const unsigned u = blockIdx.x * kBlock + threadIdx.x, row = u / per_row;
+    const int b = blockIdx.y / a.c.heads, g = blockIdx.y % a.c.heads;
+    const int rows = a.count ? min(a.count[b], a.rows) : a.rows;
+    if ((int)row >= rows) return;
+    const long pos = (long)a.start[b] + row;
+    const int page = page_of(a.c, b, pos);
+    if (page < 0) return;
+    const int at = (u - row * per_row) * VEC;
+    const size_t party = (size_t)a.batch * a.c.heads * a.rows * a.c.dim;
+    const size_t from = ((size_t)blockIdx.y * a.rows + row) * a.c.dim + at;
+    const T *x = a.x[blockIdx.z], *m = a.b[blockIdx.z];
+    Vec<T> xv[NP], mv[NP], f;
+#pragma unroll
+    for (int i = 0; i < NP; ++i) {
+        xv[i] = *(const Vec<T> *)(x + i * party + from);
+        mv[i] = *(const Vec<T> *)(m + i * party + from);
+    }
+#pragma unroll
+    for (int k = 0; k < VEC; ++k) {
+        f.e[k] = 0;
+#pragma unroll
+        for (int i = 0; i < NP; ++i) f.e[k] += xv[i].e[k] - mv[i].e[k];
+        mv[0].e[k] += f.e[k];
+    }
+    T *to = a.pool[blockIdx.z] + row_at(a.c, 0, page, g, pos) + at;
+    const size_t slot = ((size_t)a.c.pages * a.c.heads << a.c.shift) * a.c.dim;
+    *(Vec<T> *)to = f;
+#pragma unroll
+    for (int i = 0; i < NP; ++i) *(Vec<T> *)(to + (i + 1) * slot) = mv[i];
+}
+
+// A page of one slot is contiguous over its heads.  blockIdx.y = pair, blockIdx.z = slot and pool; a thread moves kCopy vectors a block apart.
+constexpr int kCopy = 4;
+template <class T>
+__global__ __launch_bounds__(kBlock) void copy_kernel(CacheView c, const int32_t *src, const int32_t *dst, T *K, T *V)
+{
+    const int from = src[blockIdx.y], to = dst[blockIdx.y];
+    if ((unsigned)from >= (unsigned)c.pages || (unsigned)to >= (unsigned)c.pages) return;
+    const size_t words = ((size_t)c.heads << c.shift) * c.dim, vecs = words / (16 / sizeof(T));
+    T *pool = (blockIdx.z & 1 ? V : K) + (blockIdx.z >> 1) * words * c.pages;
+    const Vec<T> *in = (const Vec<T> *)(pool + from * words);
+    Vec<T> *out = (Vec<T> *)(pool + to * words), v[kCopy];
+    const size_t first = (size_t)blockIdx.x * (kBlock * kCopy) + threadIdx.x;
+#pragma unroll
+    for (int k = 0; k < kCopy; ++k)
+        if (first + k * kBlock < vecs) v[k] = in[first + k * kBlock];
+#pragma unroll
+    for (int k = 0; k < kCopy; ++k)
+        if (first + k * kBlock < vecs) out[first + k * kBlock] = v[k];
+}
+
+// One thread: 16 bytes of one head and slot of all kept rows, kAhead rows read before the first of them is written.  kept ascends, so a row
+// is written only where no later row is read from: j <= kept[j] < kept[j + 1].  blockIdx.y = sequence, blockIdx.z = slot and pool.
+constexpr int kAhead = 8;
+template <class T>
+__global__ __launch_bounds__(kBlock) void compact_kernel(CacheView c, int nodes, const int32_t *context, const int32_t *kept, const int32_t *kept_count, T *K, T *V)
+{
+    constexpr int VEC = 16 / sizeof(T);
+    const unsigned per_row = c.dim / VEC, u = blockIdx.x * kBlock + threadIdx.x;
+    const int g = u / per_row, at = (u - g * per_row) * VEC, b = blockIdx.y, slot = blockIdx.z >> 1;
+    const int first = context[b], count = min(kept_count[b], nodes);
+    if (g >= c.heads || first < 0) return;
+    T *pool = blockIdx.z & 1 ? V : K;
+    for (int j = 0; j < count; j += kAhead) {
+        Vec<T> v[kAhead];
+        bool there[kAhead];
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) {
+            const int node = j + k < count ? kept[(size_t)b * nodes + j + k] : -1;
+            const int page = node >= 0 && node < nodes ? page_of(c, b, (long)first + node) : -1;
+            there[k] = page >= 0;
+            if (there[k]) v[k] = *(const Vec<T> *)(pool + row_at(c, slot, page, g, (long)first + node) + at);
+        }
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) {
+            const int page = there[k] ? page_of(c, b, (long)first + j + k) : -1;
+            if (page >= 0) *(Vec<T> *)(pool + row_at(c, slot, page, g, (long)first + j + k) + at) = v[k];
+        }
+    }
+}
+
+}  // namespace
+
+template <class T> spin_status launch_cache_append(const AppendArgs<T> &a, hipStream_t s)
+{
+    KernelTimer timer(SPIN_KERNEL_CACHE, s);
+    const size_t vecs = (size_t)a.rows * a.c.dim / (16 / sizeof(T));
+    const dim3 grid((unsigned)((vecs + kBlock - 1) / kBlock), a.batch * a.c.heads, 2);
+    for_party_count(a.n, [&](auto np) { append_kernel<decltype(np)::value, T><<<grid, kBlock, 0, s>>>(a); });
+    return check_launch("spin_cache_append");
+}
+
+template <class T> spin_status launch_cache_copy(const CacheView &c, int n, int pairs, const int32_t *src, const int32_t *dst, T *K, T *V, hipStream_t s)
+{
+    KernelTimer timer(SPIN_KERNEL_CACHE, s);
+    const size_t vecs = ((size_t)c.heads << c.shift) * c.dim / (16 / sizeof(T));
+    const dim3 grid((unsigned)((vecs + kBlock * kCopy - 1) / (kBlock * kCopy)), pairs, 2 * (n + 1));
+    copy_kernel<T><<<grid, kBlock, 0, s>>>(c, src, dst, K, V);
+    return check_launch("spin_cache_copy");
+}
+
+template <class T>
+spin_status launch_cache_compact(const CacheView &c, int n, int batch, int nodes, const int32_t *context, const int32_t *kept, const int32_t *kept_count,
+                                 T *K, T *V, hipStream_t s)
+{
+    KernelTimer timer(SPIN_KERNEL_CACHE, s);
+    const size_t vecs = (size_t)c.heads * c.dim / (16 / sizeof(T));
+    const dim3 grid((unsigned)((vecs + kBlock - 1) / kBlock), batch, 2 * (n + 1));
+    compact_kernel<T><<<grid, kBlock, 0, s>>>(c, nodes, context, kept, kept_count, K, V);
+    return check_launch("spin_cache_compact");
+}
+
+#define INSTANTIATE(T)                                                                                                                             \
+    template spin_status launch_cache_append<T>(const AppendArgs<T> &, hipStream_t);                                                               \
+    template spin_status launch_cache_copy<T>(const CacheView &, int, int, const int32_t *, const int32_t *, T *, T *, hipStream_t);               \
+    template spin_status launch_cache_compact<T>(const CacheView &, int, int, int, const int32_t *, const int32_t *, const int32_t *, T *, T *, hipStream_t)
+INSTANTIATE(u64);
+INSTANTIATE(u32);
+#undef INSTANTIATE
+
+}  // namespace spin

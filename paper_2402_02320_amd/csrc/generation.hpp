@@ -1,0 +1,107 @@
+// What the kernels for generating token by token share: the paged cache as kernels see it, what a drafted token sees, and the
+// truncation of shares held in registers.  Interface: spin_cache_* and spin_relbias_* in include/spin.h.
+#pragma once
+#include "common.hpp"
+
+namespace spin {
+
+struct CacheView {                     // of one pool
+    int pages, heads, dim, table_pages, shift;           // page_tokens = 1 << shift
+    const int32_t *table;
+};
+struct DraftView {                     // who sees what
+    int nodes, columns;
+    const int32_t *context;
+    const u64 *tree;
+};
+struct BiasView {
+    int buckets, reach;
+    const int32_t *bucket_of;
+    const void *table;
+};
+
+template <class T> struct AttentionArgs {
+    CacheView c;
+    DraftView d;
+    BiasView bias;                     // scores only; table null: none
+    const int32_t *depth;
+    int n, batch, heads, f;
+    const T *pool, *x, *A, *C, *r, *r_top, *r_msb;       // x: Q or P
+    T masked;
+    T *out;
+    void *workspace;
+};
+template <class T> struct AppendArgs {
+    CacheView c;
+    int n, batch, rows;
+    const int32_t *start, *count;
+    const T *x[2], *b[2];
+    T *pool[2];
+};
+template <class T> struct PairArgs {   // scores as whole matrices
+    BiasView bias;
+    int n, batch, heads, Q, K, first, causal, f;
+    const int32_t *lengths;
+    const T *x, *r, *r_top, *r_msb;
+    T masked;
+    T *out;
+};
+
+// T = u32 or u64
+template <class T> spin_status launch_cache_append(const AppendArgs<T> &a, hipStream_t s);
+template <class T> spin_status launch_cache_copy(const CacheView &c, int n, int pairs, const int32_t *src, const int32_t *dst, T *K, T *V, hipStream_t s);
+template <class T>
+spin_status launch_cache_compact(const CacheView &c, int n, int batch, int nodes, const int32_t *context, const int32_t *kept, const int32_t *kept_count,
+                                 T *K, T *V, hipStream_t s);
+template <class T> spin_status launch_cache_scores(const AttentionArgs<T> &a, hipStream_t s);
+template <class T> spin_status launch_cache_values(const AttentionArgs<T> &a, hipStream_t s);
+size_t cache_values_workspace(int n, int batch, int heads, int cached_heads, int nodes, int columns, int dim, int word_bytes);
+template <class T> spin_status launch_relbias_trunc(const PairArgs<T> &a, hipStream_t s);
+template <class T> spin_status launch_relbias_grad(const PairArgs<T> &a, hipStream_t s);
+
+namespace {
+
+// The page of position `pos` of sequence b, or -1 where there is none.  pos may be anything.
+__host__ __device__ inline int page_of(const CacheView &c, int b, long pos)
+{
+    if (pos < 0 || (pos >> c.shift) >= c.table_pages) return -1;
+    const int p = c.table[(size_t)b * c.table_pages + (pos >> c.shift)];
+    return (unsigned)p < (unsigned)c.pages ? p : -1;
+}
+// Word offset of a cached row.
+__host__ __device__ inline size_t row_at(const CacheView &c, int slot, int page, int head, long pos)
+{
+    return (((((size_t)slot * c.pages + page) * c.heads + head) << c.shift) + (pos & ((1l << c.shift) - 1))) * c.dim;
+}
+// The nodes that node m of sequence b sees, as bits.
+__host__ __device__ inline u64 tree_row(const DraftView &d, int b, int m) { return d.tree ? d.tree[(size_t)b * d.nodes + m] : ((u64)2 << m) - 1; }
+__host__ __device__ inline bool sees(u64 row, int nodes, int context, int pos)
+{
+    const long at = (long)pos - context;
+    return context >= 0 && (at < 0 || (at < nodes && (row >> at & 1)));
+}
+
+// Truncation (Section 4.4; steps as listed at spin_trunc) of one element whose shares are y[], given its tuple.
+template <int NP, class T> __device__ inline void truncate_shares(T (&y)[NP], const T (&r)[NP], const T (&r_top)[NP], const T (&r_msb)[NP], int f)
+{
+    constexpr int L = 8 * sizeof(T);
+    T c = (T)1 << (L - 2);
+#pragma unroll
+    for (int i = 0; i < NP; ++i) c += y[i] + r[i];
+    const T c_msb = c >> (L - 1), c_top = (c >> f) & (((T)1 << (L - 1 - f)) - 1);
+#pragma unroll
+    for (int i = 0; i < NP; ++i) {
+        y[i] = ((r_msb[i] - 2 * c_msb * r_msb[i]) << (L - 1 - f)) - r_top[i];
+        if (i == 0) y[i] += (c_msb << (L - 1 - f)) + c_top - ((T)1 << (L - 2 - f));
+    }
+}
+
+// Bucket of a distance, or -1 where it has none.
+__host__ __device__ inline int bucket_at(const BiasView &v, int distance)
+{
+    const int b = v.bucket_of[(distance < -v.reach ? -v.reach : distance > v.reach ? v.reach : distance) + v.reach];
+    return (unsigned)b < (unsigned)v.buckets ? b : -1;
+}
+
+}  // namespace
+}  // namespace spin

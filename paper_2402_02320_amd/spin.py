@@ -104,6 +104,13 @@ def lib():
         L.spin_matmul_grouped_by.argtypes = [_MatmulWay, i32, i32, p, p, sz, p]
         for name in ("spin_matmul_way_of", "spin_matmul_grouped_way_of", "spin_matmul_by", "spin_matmul_grouped_by"):
             getattr(L, name).restype = i32
+        for pre, word in (("spin_", u64), ("spin32_", ctypes.c_uint32)):
+            for name, argtypes in (("cache_append", [p, i32] + [p] * 7), ("cache_copy", [p, i32] + [p] * 3), ("cache_compact", [p, i32] + [p] * 4),
+                                   ("cache_scores", [p] + [i32] * 4 + [p] * 8 + [word] + [p] * 4),
+                                   ("cache_values", [p] + [i32] * 4 + [p] * 10 + [sz, p]), ("cache_values_workspace_bytes", [p] + [i32] * 3),
+                                   ("relbias_trunc", [i32] * 7 + [p, i32] + [p] * 4 + [word] + [p] * 3), ("relbias_grad", [i32] * 7 + [p] * 5)):
+                getattr(L, pre + name).argtypes = argtypes
+                getattr(L, pre + name).restype = sz if name.endswith("_bytes") else i32
         L.spin_probe_mfma.argtypes = [p, i32, i32, p, p]
         L.spin_probe_mfma.restype = i32
         L.spin_status_string.argtypes = [i32]
@@ -690,9 +697,210 @@ class ring32:
         return out
 
 
+# ---- a paged cache of shares, attention over it, relative position bias ---------------------------------------------------------
+class _Cache(ctypes.Structure):
+    _fields_ = [(k, ctypes.c_int) for k in ("n", "pages", "heads", "page_tokens", "dim")] + [("K", ctypes.c_void_p), ("V", ctypes.c_void_p)] + \
+               [("batch", ctypes.c_int), ("table_pages", ctypes.c_int), ("table", ctypes.c_void_p)]
+
+
+class _RelBias(ctypes.Structure):
+    _fields_ = [("buckets", ctypes.c_int), ("reach", ctypes.c_int), ("bucket_of", ctypes.c_void_p), ("table", ctypes.c_void_p)]
+
+
+def _list32(t, name, *shape):
+    """A device array of int32_t; its shape is checked as far as it is given (None: any length)."""
+    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype == torch.int32 and t.is_contiguous()):
+        raise SpinError("%s must be a contiguous torch.int32 CUDA tensor" % name)
+    if t.dim() != len(shape) or any(w is not None and w != k for w, k in zip(shape, t.shape)):
+        raise SpinError("%s has the shape %s" % (name, tuple(t.shape)))
+    return t.data_ptr()
+
+
+def _shapes(ok):
+    if not ok:
+        raise SpinError("inconsistent operand shapes")
+
+
+def _cache(word, K, V, table, batch):
+    """The library's description of a cache, of one pool where the other is None."""
+    pool = V if K is None else K
+    _shapes(pool.dim() == 5 and (K is None or V is None or V.shape == K.shape))
+    slots, pages, heads, tokens, dim = pool.shape
+    at = None if table is None else _list32(table, "table", batch, None)
+    return _Cache(slots - 1, pages, heads, tokens, dim, None if K is None else word.dev(K, "K"), None if V is None else word.dev(V, "V"),
+                  batch, 0 if table is None else table.shape[1], at)
+
+
+def _bias(word, bias, n, heads):
+    table, bucket_of = bias
+    _shapes(table.dim() == 3 and tuple(table.shape[:2]) == (n, heads))
+    return _bucketing(bucket_of, table.shape[2], word.dev(table, "bias"))
+
+
+def _bucketing(bucket_of, buckets, table=None):
+    if bucket_of.numel() % 2 == 0:
+        raise SpinError("bucket_of has an entry for each distance from -reach to reach")
+    return _RelBias(buckets, bucket_of.numel() // 2, _list32(bucket_of, "bucket_of", None), table)
+
+
+def _tuple_ptrs(word, tuple_, f, shape):
+    if not f:
+        return None, None, None
+    if tuple_ is None:
+        raise SpinError("a truncation needs its tuple (r, r_top, r_msb)")
+    _shapes(all(t.shape == shape for t in tuple_))
+    return tuple(word.dev(t, k) for t, k in zip(tuple_, ("r", "r_top", "r_msb")))
+
+
+class _Word:
+    """The calls that exist for 64- and 32-bit words, of one of them."""
+
+    def __init__(self, bits):
+        self.bits, self.prefix = bits, "spin_" if bits == 64 else "spin32_"
+
+    def dev(self, t, name):
+        return _dev(t, name) if self.bits == 64 else _dev32(t, name)
+
+    def out(self, t, name, words):
+        return _dev_out(t, name, words) if self.bits == 64 else _dev32_out(t, name, words)
+
+    def entry(self, name):
+        return getattr(lib(), self.prefix + name)
+
+    def cache_append(self, pools, table, start, x, b, count=None):
+        """Opens new rows of keys and values, x = (keys, values), against their masks b = (for keys, for values), all
+        [n, batch, heads, rows, dim], and writes them into pools = (K, V), [n + 1, pages, heads, page tokens, dim]: row s of sequence b at
+        position start[b] + s, on the page table[b, position // page tokens].  count: rows of every sequence, if not all.  Returns pools."""
+        (K, V), (Kx, Vx), (Kb, Vb) = pools, x, b
+        _shapes(Kx.dim() == 5 and all(t.shape == Kx.shape for t in (Vx, Kb, Vb)))
+        n, batch, heads, rows, dim = Kx.shape
+        c = _cache(self, K, V, table, batch)
+        _shapes((c.n, c.heads, c.dim) == (n, heads, dim))
+        _check(self.entry("cache_append")(ctypes.byref(c), rows, _list32(start, "start", batch), None if count is None else _list32(count, "count", batch),
+                                          self.dev(Kx, "x"), self.dev(Kb, "b"), self.dev(Vx, "x"), self.dev(Vb, "b"), _stream()))
+        return pools
+
+    def cache_copy(self, pools, src, dst):
+        """Copies pages src of both pools to pages dst (no page twice in dst, none in both).  Returns pools."""
+        c = _cache(self, pools[0], pools[1], None, 0)
+        _check(self.entry("cache_copy")(ctypes.byref(c), src.numel(), _list32(src, "src", None), _list32(dst, "dst", src.numel()), _stream()))
+        return pools
+
+    def cache_compact(self, pools, table, context, kept, kept_count):
+        """Keeps kept[b, :kept_count[b]], ascending, of the drafted tokens that stand at position context[b] and on: their rows move together
+        to context[b] and on.  kept: [batch, nodes].  Returns pools."""
+        _shapes(kept.dim() == 2)
+        batch, nodes = kept.shape
+        c = _cache(self, pools[0], pools[1], table, batch)
+        _check(self.entry("cache_compact")(ctypes.byref(c), nodes, _list32(context, "context", batch), _list32(kept, "kept", batch, nodes),
+                                           _list32(kept_count, "kept_count", batch), _stream()))
+        return pools
+
+    @staticmethod
+    def _tree(tree, batch, nodes):
+        if tree is None:
+            return None
+        if not (tree.is_cuda and tree.dtype == torch.int64 and tree.is_contiguous()):
+            raise SpinError("tree must be a contiguous torch.int64 CUDA tensor")
+        _shapes(tuple(tree.shape) == (batch, nodes))
+        return tree.data_ptr()
+
+    def cache_scores(self, K, table, context, Q, A, C, f=0, tuple_=None, tree=None, masked=0, bias=None, depth=None, out=None):
+        """Scores of the new tokens of every sequence, which stand in the cache at context[b] and on, over what they see of it.
+        K: pool; Q, A: [n, batch, query heads, nodes, dim]; C, the truncation tuple and the result: [n, batch, query heads, nodes, columns].
+        tree[b, m]: bits of the drafted tokens that node m sees (None: those up to itself).  masked: public word where nothing is seen.
+        bias: (table [n, query heads, buckets], bucket_of) is added after truncation, distances by depth[b, m] behind the context."""
+        _shapes(Q.dim() == 5 and A.shape == Q.shape and C.dim() == 5 and C.shape[:4] == Q.shape[:4])
+        n, batch, heads, nodes, dim = Q.shape
+        c = _cache(self, K, None, table, batch)
+        _shapes((c.n, c.dim) == (n, dim))
+        r, r_top, r_msb = _tuple_ptrs(self, tuple_, f, C.shape)
+        if out is None:
+            out = torch.empty_like(C)
+        _check(self.entry("cache_scores")(ctypes.byref(c), heads, nodes, C.shape[4], f, _list32(context, "context", batch), self._tree(tree, batch, nodes),
+                                          self.dev(Q, "Q"), self.dev(A, "A"), self.dev(C, "C"), r, r_top, r_msb, masked % (1 << self.bits),
+                                          None if bias is None else ctypes.byref(_bias(self, bias, n, heads)),
+                                          None if bias is None or depth is None else _list32(depth, "depth", batch, nodes),
+                                          self.out(out, "out", C.numel()), _stream()))
+        return out
+
+    def cache_values_workspace_bytes(self, V, table, heads, nodes, columns):
+        slots, pages, cached, tokens, dim = V.shape
+        c = _Cache(slots - 1, pages, cached, tokens, dim, None, None, table.shape[0], table.shape[1], table.data_ptr())
+        return int(self.entry("cache_values_workspace_bytes")(ctypes.byref(c), heads, nodes, columns))
+
+    def cache_values(self, V, table, context, P, A, C, f=0, tuple_=None, tree=None, out=None, workspace=None):
+        """Sums of the cached values that the new tokens see, weighted by P.  V: pool; P, A: [n, batch, query heads, nodes, columns];
+        C, the truncation tuple and the result: [n, batch, query heads, nodes, dim].  Everything else as for cache_scores."""
+        _shapes(P.dim() == 5 and A.shape == P.shape and C.dim() == 5 and C.shape[:4] == P.shape[:4])
+        n, batch, heads, nodes, columns = P.shape
+        c = _cache(self, None, V, table, batch)
+        _shapes((c.n, c.dim) == (n, C.shape[4]))
+        r, r_top, r_msb = _tuple_ptrs(self, tuple_, f, C.shape)
+        if out is None:
+            out = torch.empty_like(C)
+        if workspace is None:
+            size = int(self.entry("cache_values_workspace_bytes")(ctypes.byref(c), heads, nodes, columns))
+            if size == 0:
+                raise SpinError("invalid cache or attention dimensions")
+            workspace = torch.empty(size, dtype=torch.uint8, device=P.device)
+        _check(self.entry("cache_values")(ctypes.byref(c), heads, nodes, columns, f, _list32(context, "context", batch), self._tree(tree, batch, nodes),
+                                          self.dev(P, "P"), self.dev(A, "A"), self.dev(C, "C"), r, r_top, r_msb, self.out(out, "out", C.numel()),
+                                          _workspace_ptr(workspace), workspace.numel() * workspace.element_size(), _stream()))
+        return out
+
+    def relbias_trunc(self, x, bias, bucket_of, f=0, tuple_=None, first=0, causal=False, lengths=None, masked=0, out=None):
+        """Scores x [n, batch, heads, Q, K] truncated by f bits plus bias[n, heads, buckets] at the bucket of k - (q + first); `masked` where
+        k >= lengths[batch] or, if causal, k > q + first."""
+        _shapes(x.dim() == 5)
+        n, batch, heads, Q, K = x.shape
+        v = _bias(self, (bias, bucket_of), n, heads)
+        r, r_top, r_msb = _tuple_ptrs(self, tuple_, f, x.shape)
+        if out is None:
+            out = torch.empty_like(x)
+        _check(self.entry("relbias_trunc")(n, batch, heads, Q, K, first, 1 if causal else 0, None if lengths is None else _list32(lengths, "lengths", batch), f,
+                                           self.dev(x, "x"), r, r_top, r_msb, masked % (1 << self.bits), ctypes.byref(v), self.out(out, "out", x.numel()), _stream()))
+        return out
+
+    def relbias_grad(self, dS, bucket_of, buckets, first=0, causal=False, lengths=None, out=None):
+        """Gradient [n, heads, buckets] of the bias of relbias_trunc from that of its result, dS [n, batch, heads, Q, K]."""
+        _shapes(dS.dim() == 5)
+        n, batch, heads, Q, K = dS.shape
+        v = _bucketing(bucket_of, buckets)
+        if out is None:
+            out = torch.empty((n, heads, buckets), dtype=dS.dtype, device=dS.device)
+        _check(self.entry("relbias_grad")(n, batch, heads, Q, K, first, 1 if causal else 0, None if lengths is None else _list32(lengths, "lengths", batch),
+                                          self.dev(dS, "dS"), ctypes.byref(v), self.out(out, "grad", n * heads * buckets), _stream()))
+        return out
+
+
+_CALLS_BY_WORD = ("cache_append", "cache_copy", "cache_compact", "cache_scores", "cache_values", "cache_values_workspace_bytes", "relbias_trunc", "relbias_grad")
+for _name in _CALLS_BY_WORD:
+    globals()[_name] = getattr(_Word(64), _name)
+    setattr(ring32, _name, staticmethod(getattr(_Word(32), _name)))
+
+
+def relative_buckets(buckets, reach, both_ways):
+    """bucket_of for the bias calls (on the CPU): of the distances key - query from -reach to reach, the near ones have a bucket each and the
+    far ones share logarithmic ranges, the last of which holds all from `reach` on.  both_ways: half of the buckets are for keys after the query;
+    otherwise those share bucket 0.  The ranges' borders near * (reach / near)^(j / wide) are compared in whole numbers."""
+    half = buckets // 2 if both_ways else buckets
+    near = half // 2
+    wide = half - near
+    if near < 1 or reach <= near or (both_ways and buckets % 2):
+        raise SpinError("relative_buckets: at least two buckets a direction and a reach beyond the near ones")
+
+    def of(d):
+        if d < near:
+            return d
+        return near + max(j for j in range(wide) if d ** wide * near ** j >= reach ** j * near ** wide)
+    return torch.tensor([(half if both_ways and d > 0 else 0) + of(abs(d) if both_ways else max(-d, 0)) for d in range(-reach, reach + 1)],
+                        dtype=torch.int32)
+
+
 KERNELS = {"random": 0, "share": 1, "open": 2, "beaver_mul": 3, "trunc": 4, "pack": 5, "gemm_limb": 6,
            "gemm_valu": 7, "lincomb": 8, "binary": 9, "cast": 10, "probe": 11, "beaver_mul_trunc": 12,
-           "gemm_residue": 13, "combine": 14, "gemm_direct": 15}
+           "gemm_residue": 13, "combine": 14, "gemm_direct": 15, "cache": 16, "attention": 17, "relbias": 18}
 
 
 def probe_mfma(operands, blocks, iters, sink=None):
