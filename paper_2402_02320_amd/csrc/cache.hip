@@ -78,20 +78,18 @@ __global__ __launch_bounds__(kBlock) void compact_kernel(CacheView c, int nodes,
     if (g >= c.heads || first < 0) return;
     T *pool = blockIdx.z & 1 ? V : K;
     for (int j = 0; j < count; j += kAhead) {
-        Vec<T> v[kAhead];
-        bool there[kAhead];
+        u32x4 v[kAhead];
+        int page[kAhead];                                  // to write to
 #pragma unroll
         for (int k = 0; k < kAhead; ++k) {
             const int node = j + k < count ? kept[(size_t)b * nodes + j + k] : -1;
-            const int page = node >= 0 && node < nodes ? page_of(c, b, (long)first + node) : -1;
-            there[k] = page >= 0;
-            if (there[k]) v[k] = *(const Vec<T> *)(pool + row_at(c, slot, page, g, (long)first + node) + at);
+            const int from = node >= 0 && node < nodes ? page_of(c, b, (long)first + node) : -1;
+            page[k] = from >= 0 ? page_of(c, b, (long)first + j + k) : -1;
+            v[k] = *(const u32x4 *)(pool + row_at(c, slot, max(from, 0), g, from >= 0 ? (long)first + node : 0) + at);
         }
 #pragma unroll
-        for (int k = 0; k < kAhead; ++k) {
-            const int page = there[k] ? page_of(c, b, (long)first + j + k) : -1;
-            if (page >= 0) *(Vec<T> *)(pool + row_at(c, slot, page, g, (long)first + j + k) + at) = v[k];
-        }
+        for (int k = 0; k < kAhead; ++k)
+            if (page[k] >= 0) *(u32x4 *)(pool + row_at(c, slot, page[k], g, (long)first + j + k) + at) = v[k];
     }
 }
 

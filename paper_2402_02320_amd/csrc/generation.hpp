@@ -81,19 +81,26 @@ __host__ __device__ inline bool sees(u64 row, int nodes, int context, int pos)
     return context >= 0 && (at < 0 || (at < nodes && (row >> at & 1)));
 }
 
-// Truncation (Section 4.4; steps as listed at spin_trunc) of one element whose shares are y[], given its tuple.
+// Truncation (Section 4.4; steps as listed at spin_trunc) of one element: every party's y + r is added to the opened value, which then tells every
+// party its share of the result.
+template <class T> struct Opened {
+    static constexpr int L = 8 * sizeof(T);
+    int f;
+    T c = (T)1 << (L - 2);
+    __device__ void add(T masked) { c += masked; }
+    __device__ T truncated(int party, T r_top, T r_msb) const
+    {
+        const T c_msb = c >> (L - 1), y = ((r_msb - 2 * c_msb * r_msb) << (L - 1 - f)) - r_top;
+        return party ? y : y + (c_msb << (L - 1 - f)) + ((c >> f) & (((T)1 << (L - 1 - f)) - 1)) - ((T)1 << (L - 2 - f));
+    }
+};
 template <int NP, class T> __device__ inline void truncate_shares(T (&y)[NP], const T (&r)[NP], const T (&r_top)[NP], const T (&r_msb)[NP], int f)
 {
-    constexpr int L = 8 * sizeof(T);
-    T c = (T)1 << (L - 2);
+    Opened<T> c{f};
 #pragma unroll
-    for (int i = 0; i < NP; ++i) c += y[i] + r[i];
-    const T c_msb = c >> (L - 1), c_top = (c >> f) & (((T)1 << (L - 1 - f)) - 1);
+    for (int i = 0; i < NP; ++i) c.add(y[i] + r[i]);
 #pragma unroll
-    for (int i = 0; i < NP; ++i) {
-        y[i] = ((r_msb[i] - 2 * c_msb * r_msb[i]) << (L - 1 - f)) - r_top[i];
-        if (i == 0) y[i] += (c_msb << (L - 1 - f)) + c_top - ((T)1 << (L - 2 - f));
-    }
+    for (int i = 0; i < NP; ++i) y[i] = c.truncated(i, r_top[i], r_msb[i]);
 }
 
 // Bucket of a distance, or -1 where it has none.
