@@ -6,7 +6,7 @@
 // fragment may be any 16 as long as both factors take the same, so they are those that its 16-byte loads bring,
 //     k(j, h, e) = 4 W j + W h + e       (W words in 16 bytes, h = lane / 16, e < W),
 // which makes the four lanes of a row read 64 bytes side by side.  The new tokens' factor (E and every A_i, 16 rows) is split once a workgroup
-// into LDS, in fragment order.  All parties' products stay in the registers of one wave, so the truncation needs no second pass.
+// into LDS, in fragment order.
 #include "generation.hpp"
 #include "limb_common.hpp"
 
@@ -15,6 +15,7 @@ namespace {
 
 constexpr int kTile = 16;              // query rows, and cached rows (scores) or columns (values), of one MFMA
 constexpr int kDepth = 64;             // k of one MFMA
+constexpr int kXcds = 8;               // workgroups go to the XCDs in turn
 
 template <class T> struct Lane {
     static constexpr int ND = sizeof(T), W = 16 / sizeof(T), loads = 16 / W;
@@ -68,15 +69,24 @@ __device__ inline void put_digits(char *frag, int lane, int q, const u32 (&w)[4]
     *(u32 *)(at + 3 * kFrag) = __builtin_amdgcn_perm(t3, t1, 0x07060302u);
 }
 
-// acc += left . right over all digit pairs that count; left: ND fragments in LDS, this lane's 16 bytes of the first at `left`.
-template <class T> __device__ inline void multiply(v4i (&acc)[sizeof(T)], const char *left, const v4i (&right)[sizeof(T)])
+// acc += left0 . right0 + left1 . right1 over all digit pairs that count; left: ND fragments in LDS, this lane's 16 bytes of the first.  One fragment is read
+// ahead: left alone the compiler reads all of them first, into 64 registers.
+template <class T> __device__ inline void multiply(v4i (&acc)[sizeof(T)], const char *left0, const v4i (&right0)[sizeof(T)], const char *left1, const v4i (&right1)[sizeof(T)])
 {
+    constexpr int ND = sizeof(T);
+    v4i ahead = *(const v4i *)left0;
 #pragma unroll
-    for (int j = 0; j < (int)sizeof(T); ++j) {
-        const v4i a = *(const v4i *)(left + j * kFrag);
+    for (int p = 0; p < 2 * ND; ++p) {
+        const v4i a = ahead;
+        if (p + 1 < 2 * ND) ahead = *(const v4i *)(p + 1 < ND ? left0 + (p + 1) * kFrag : left1 + (p + 1 - ND) * kFrag);
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int i = 0; i + j < (int)sizeof(T); ++i) acc[i + j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(a, right[i], acc[i + j], 0, 0, 0);
+        for (int i = 0; i + p % ND < ND; ++i)
+            acc[i + p % ND] = __builtin_amdgcn_mfma_i32_16x16x64_i8(a, p < ND ? right0[i] : right1[i], acc[i + p % ND], 0, 0, 0);
     }
+    // Multiplied here: put off to where the sums are used, the fragments of all parties would be kept until then.
+#pragma unroll
+    for (int d = 0; d < ND; ++d) asm volatile("" : "+v"(acc[d]));
 }
 
 // The word whose diagonals are acc[..][r].
@@ -88,25 +98,50 @@ template <class T> __device__ inline T recombine(const v4i (&acc)[sizeof(T)], in
     return v;
 }
 
+// The run or range of tokens and the first row of a workgroup.  Row tiles of one run are eight workgroup ids apart: on one XCD, next to each other in time, so
+// that its L2 serves all but the first.  Which XCD has a run goes round with the head and the sequence: short sequences have the first runs only.
+__device__ inline void place_of(int row_tiles, int &block, int &row0)
+{
+    const int strip = blockIdx.x / (kXcds * row_tiles), within = blockIdx.x % (kXcds * row_tiles);
+    block = strip * kXcds + (within + blockIdx.y + blockIdx.z * gridDim.y) % kXcds;
+    row0 = within / kXcds * kTile;
+}
+
+// A word at a scalar address and a lane's bytes from there (rows have at most kMostColumns words, so 16 of them are within 2^31 bytes): no register a lane but
+// those 32 bits goes into addresses.
+template <class T> __device__ inline T at_bytes(const T *scalar, u32 bytes) { return *(const T *)((const char *)scalar + bytes); }
+template <class T> __device__ inline void put_at_bytes(T *scalar, u32 bytes, T v) { *(T *)((char *)scalar + bytes) = v; }
+
 // ---- scores -----------------------------------------------------------------------------------------------------
-// A workgroup: 16 rows (query heads of one cached head, times nodes) against runs of 64 cached tokens, 16 a wave.  One k-tile of 64 elements after another;
-// `held` k-tiles of the rows' digits are in LDS: all of them, or (heads so long and parties so many that they do not fit) the one at hand.
+// A workgroup: 16 rows (query heads of one cached head, times nodes) against runs of 64 cached tokens, 16 a wave, one k-tile of 64 elements after
+// another; `held` k-tiles of the rows' digits are in LDS: all of them, or (heads so long and parties so many that they do not fit) the one at hand.
+//
+// Every party's two products go into the same diagonals where the result is truncated (SUM): what the parties open is the sum of their masked shares,
+// and no share of Z is asked for by itself.  (8 pairs x 2 products x 256 elements x 8 parties x 2^14 = 2^29 fits an int32.)  Without truncation a workgroup
+// has one party.
+//
+// HBM bounds it (a tile of 16 rows of three parties takes 64 KB of cache and 432 MFMA, a sixth of the time), if enough is in flight: a wave has the loads of
+// two slots in flight, over the ends of k-tiles and runs, and reads all of a score's triple and tuple words at once.
 constexpr int kScoreWaves = 4, kScoreBlock = 64 * kScoreWaves;
 
-template <int NP, class T>
-__global__ __launch_bounds__(kScoreBlock, NP * (int)sizeof(T) <= 40 ? 2 : 1) void scores_kernel(AttentionArgs<T> a, int runs, int held)
+template <int NP, class T, bool SUM>
+__global__ __launch_bounds__(kScoreBlock, sizeof(T) == 8 ? 2 : NP < 6 ? 4 : 3) void scores_kernel(AttentionArgs<T> a, int runs, int held)
 {
     using L = Lane<T>;
-    constexpr int ND = L::ND, W = L::W;
+    constexpr int ND = L::ND, W = L::W, STEPS = SUM ? NP + 1 : 2;
     typedef T vec __attribute__((ext_vector_type(L::W)));
     extern __shared__ __align__(16) char lds[];
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), h = lane / 16;
-    const int b = blockIdx.z, share = a.heads / a.c.heads, R = share * a.d.nodes, row_tiles = (R + kTile - 1) / kTile;
-    const int g = blockIdx.y / row_tiles, row0 = blockIdx.y % row_tiles * kTile;
+    const int b = SUM ? blockIdx.z : blockIdx.z / NP, party = SUM ? 0 : blockIdx.z % NP;
+    const int share = a.heads / a.c.heads, R = share * a.d.nodes, row_tiles = (R + kTile - 1) / kTile;
+    int block, row0;
+    place_of(row_tiles, block, row0);
+    const int g = blockIdx.y;
     const size_t rows = (size_t)a.batch * a.heads * a.d.nodes, first_row = ((size_t)b * a.heads + (size_t)g * share) * a.d.nodes + row0;
     const int context = a.d.context[b], dim = a.c.dim;
     const int limit = context < 0 ? 0 : (int)min((long)a.d.columns, (long)context + a.d.nodes);
-    const int k_tiles = (dim + kDepth - 1) / kDepth;
+    const int k_tiles = (dim + kDepth - 1) / kDepth, begin = block * runs * kDepth;
+    if (begin >= a.d.columns) return;
 
     auto stage = [&](int kt0, int count) __attribute__((always_inline)) {                // digits of E and A_i of k-tiles kt0 .. kt0 + count - 1
         const int per_row = count * (kDepth / W);
@@ -139,304 +174,358 @@ __global__ __launch_bounds__(kScoreBlock, NP * (int)sizeof(T) <= 40 ? 2 : 1) voi
             }
         }
     };
-    const bool whole = held >= k_tiles;
-    if (whole && blockIdx.x * (runs * kDepth) < (unsigned)limit) {
-        stage(0, k_tiles);
-        __syncthreads();
-    }
     const size_t slot = ((size_t)a.c.pages * a.c.heads << a.c.shift) * dim;
-    for (int run = 0; run < runs; ++run) {
-        const int first = (blockIdx.x * runs + run) * (kScoreWaves * kTile);
-        if (first >= a.d.columns) break;                   // of the whole workgroup
-        const int t0 = first + wave * kTile, t = t0 + lane % 16;
-        const int page = page_of(a.c, b, t);
-        T z[NP][4];
+    const T *slots = a.pool + (SUM ? 0 : party * slot);    // the one that party's slot comes after
+    const u32 lane_row = lane % 16 * dim * sizeof(T), lane_at = lane_row + h * W * sizeof(T);  // 16 tokens are on one page: a scalar address and these bytes
+    vec raw[2][L::loads];
+    // The words of a step; past a row's end the rows' digits are zero, whatever is read.  No load stands behind a branch: its register would be copied where the
+    // branches meet, and a copy waits for the load.
+    auto load = [&](vec (&v)[L::loads], int s, int kt, size_t key) __attribute__((always_inline)) {
+        const char *from = (const char *)((s == 0 ? a.pool : slots + s * slot) + key);
+        int begin_of = kt * kDepth;
+        asm volatile("" : "+s"(begin_of));                 // addresses are made here, not carried along for every slot and j
 #pragma unroll
-        for (int i = 0; i < NP; ++i)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) z[i][r] = 0;
-        if (first < limit) {                               // of the whole workgroup
-            const T *key = a.pool + row_at(a.c, 0, max(page, 0), g, page < 0 ? 0 : t) + h * W;
-            for (int kt = 0; kt < k_tiles; ++kt) {
-                if (!whole) {
-                    __syncthreads();
-                    stage(kt, 1);
-                    __syncthreads();
-                }
-                const char *left = lds + (whole ? kt : 0) * (ND * kFrag) + lane * 16;
-                const bool full = (kt + 1) * kDepth <= dim;
-                vec raw[L::loads];
-                auto load = [&](int s) __attribute__((always_inline)) {
-                    const T *from = key + (s * slot + kt * kDepth);
-                    if (full) {
-#pragma unroll
-                        for (int j = 0; j < L::loads; ++j) raw[j] = *(const vec *)(from + j * (4 * W));
-                    } else {                               // past the row's end the rows' digits are zero, whatever is read
-#pragma unroll
-                        for (int j = 0; j < L::loads; ++j) raw[j] = *(const vec *)(kt * kDepth + j * (4 * W) + h * W < dim ? from + j * (4 * W) : key + s * slot);
-                    }
-                };
-                // A slot's words are split into fragments before its products, which leaves their registers to the next slot's loads.
-                auto take = [&](v4i (&p)[ND]) __attribute__((always_inline)) {
-                    T w[16];
-#pragma unroll
-                    for (int j = 0; j < 16; ++j) w[j] = raw[j / W][j % W];
-                    split<T>(w, p);
-                };
-                v4i f[ND];
-                load(0);
-                take(f);
-                load(1);
-#pragma unroll
-                for (int i = 0; i < NP; ++i) {
-                    v4i right[ND], acc[ND];
-#pragma unroll
-                    for (int d = 0; d < ND; ++d) acc[d] = v4i{0, 0, 0, 0};
-                    take(right);
-                    __builtin_amdgcn_sched_barrier(0);
-                    if (i + 1 < NP) load(i + 2);
-                    __builtin_amdgcn_sched_barrier(0);
-                    multiply<T>(acc, left, right);
-                    multiply<T>(acc, left + (i + 1) * held * (ND * kFrag), f);
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        z[i][r] += recombine<T>(acc, r);
-                        computed_here(z[i][r]);            // not at the end, with all parties' diagonals kept until then
-                    }
-                }
-            }
+        for (int j = 0; j < L::loads; ++j) {
+            const int at = begin_of + j * (4 * W);         // a row's end is a multiple of 8
+            v[j] = *(const vec *)(from + (at < dim ? at : 0) * sizeof(T) + (4 * W <= 8 || at + h * W < dim ? lane_at : lane_row));
         }
-        // row 4 h + r, token t
+    };
+    int page = 0;
+    auto key_of = [&](int first) __attribute__((always_inline)) {                        // where this wave's tile starts in slot 0
+        const int t0 = first + wave * kTile;
+        page = __builtin_amdgcn_readfirstlane(page_of(a.c, b, t0));
+        return row_at(a.c, 0, max(page, 0), g, t0);
+    };
+    const bool whole = held >= k_tiles;
+    const int active = begin < limit ? min(runs, (limit - begin + kDepth - 1) / kDepth) : 0;   // runs with something to see
+    size_t key = 0;
+    if (active) {
+        key = key_of(begin);
+        load(raw[0], 0, 0, key);
+        load(raw[1], 1, 0, key);
+        if (whole) {
+            stage(0, k_tiles);
+            __syncthreads();
+        }
+    }
+    v4i acc[ND];
+#pragma unroll
+    for (int d = 0; d < ND; ++d) acc[d] = v4i{0, 0, 0, 0};
+    int kt = 0, here = page;
+    size_t next = 0;
+    // One loop over k-tiles and runs, so that the loads of the next k-tile's first two steps are under way whichever run it belongs to; behind the last one
+    // they read the pool's first rows, which every workgroup does.  Two buffers serve any number of steps: with an odd one the last step's is filled a
+    // step before it is needed, the others' two.
+    for (int run = 0; run < active;) {
+        if (kt == 0) {
+            here = page;
+            next = run + 1 < active ? key_of(begin + (run + 1) * kDepth) : 0;
+        }
+        const int kt1 = kt + 1 == k_tiles ? 0 : kt + 1;
+        const size_t key1 = kt1 ? key : next;
+        if (!whole) {
+            __syncthreads();
+            stage(kt, 1);
+            __syncthreads();
+        }
+        const char *left = lds + (whole ? kt : 0) * (ND * kFrag) + lane * 16;
+        v4i f[ND], right[ND];
+#pragma unroll
+        for (int s = 0; s < STEPS; ++s) {
+            T w[16];
+#pragma unroll
+            for (int j = 0; j < 16; ++j) w[j] = raw[s % 2][j / W][j % W];
+            split<T>(w, s == 0 ? f : right);
+            __builtin_amdgcn_sched_barrier(0);             // these registers are the loads' of two steps on
+            if (s + 2 < STEPS) load(raw[s % 2], s + 2, kt, key);
+            else load(raw[s % 2], s % 2, kt1, key1);
+            __builtin_amdgcn_sched_barrier(0);
+            if (s > 0) multiply<T>(acc, left, right, left + (SUM ? s : party + 1) * held * (ND * kFrag), f);
+        }
+        kt = kt1;
+        if (kt) continue;
+        key = next;
+        const int t0 = begin + run * kDepth + wave * kTile, t = t0 + lane % 16, near = min(t0, a.d.columns - 1);
+        const size_t each = rows * a.d.columns, corner = first_row * a.d.columns + near;
+        ++run;
+        // Rows quarter + r, token t.  What these make of the rows is computed anew for every run: kept over the products it takes 50 registers.
+        int quarter = 4 * h;
+        asm volatile("" : "+v"(quarter));
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-            __builtin_amdgcn_sched_barrier(0);
-            const int row = row0 + 4 * h + r, m = row % a.d.nodes;
-            if (row >= R || t >= a.d.columns) continue;
-            const size_t at = (first_row + 4 * h + r) * a.d.columns + t, party = rows * a.d.columns;
-            if (page < 0 || !sees(tree_row(a.d, b, m), a.d.nodes, context, t)) {
-#pragma unroll
-                for (int i = 0; i < NP; ++i) a.out[i * party + at] = i == 0 ? a.masked : 0;
-                continue;
-            }
+            if (NP > 3) __builtin_amdgcn_sched_barrier(0); // a score's words at a time
+            const int row = row0 + quarter + r, m = row % a.d.nodes;
+            const bool mine = row < R && t < a.d.columns, seen = mine && here >= 0 && sees(tree_row(a.d, b, mine ? m : 0), a.d.nodes, context, t);
+            const u32 at = mine ? ((u32)(quarter + r) * a.d.columns + (t - near)) * sizeof(T) : 0;
             int bucket = -1;
             const T *bias = (const T *)a.bias.table + (size_t)(g * share + row / a.d.nodes) * a.bias.buckets;
-            if (a.bias.table) {
+            if (a.bias.table && seen) {
                 auto place = [&](int node) { return a.depth ? a.depth[(size_t)b * a.d.nodes + node] : node; };
                 const long away = (t < context ? (long)t - context : place(t - context)) - (long)place(m);
                 bucket = bucket_at(a.bias, (int)min(max(away, -(long)a.bias.reach), (long)a.bias.reach));
             }
-            Opened<T> c{a.f};
+            T z = recombine<T>(acc, r);
+            if constexpr (SUM) {
+                Opened<T> c{a.f};
+                c.add(z);
+                T top[NP], msb[NP];
 #pragma unroll
-            for (int i = 0; i < NP; ++i) {
-                z[i][r] += a.C[i * party + at];
-                if (a.f) c.add(z[i][r] + a.r[i * party + at]);
-            }
+                for (int i = 0; i < NP; ++i) {
+                    c.add(at_bytes(a.C + (i * each + corner), at) + at_bytes(a.r + (i * each + corner), at));
+                    top[i] = at_bytes(a.r_top + (i * each + corner), at);
+                    msb[i] = at_bytes(a.r_msb + (i * each + corner), at);
+                }
 #pragma unroll
-            for (int i = 0; i < NP; ++i) {
-                T y = a.f ? c.truncated(i, a.r_top[i * party + at], a.r_msb[i * party + at]) : z[i][r];
-                if (bucket >= 0) y += bias[(size_t)i * a.heads * a.bias.buckets + bucket];
-                a.out[i * party + at] = y;
+                for (int i = 0; i < NP; ++i) {
+                    T y = c.truncated(i, top[i], msb[i]);
+                    if (bucket >= 0) y += bias[(size_t)i * a.heads * a.bias.buckets + bucket];
+                    if (mine) put_at_bytes(a.out + (i * each + corner), at, seen ? y : i == 0 ? a.masked : 0);
+                }
+            } else if (mine) {
+                z += at_bytes(a.C + (party * each + corner), at);
+                if (bucket >= 0) z += bias[(size_t)party * a.heads * a.bias.buckets + bucket];
+                put_at_bytes(a.out + (party * each + corner), at, seen ? z : party == 0 ? a.masked : 0);
             }
+        }
+#pragma unroll
+        for (int d = 0; d < ND; ++d) acc[d] = v4i{0, 0, 0, 0};
+    }
+    // Runs that nothing of is seen.
+    const int left_over = min(a.d.columns, begin + runs * kDepth) - (begin + active * kDepth);
+    for (int c = threadIdx.x; c < left_over * min(kTile, R - row0); c += kScoreBlock) {
+        const size_t at = (first_row + c / left_over) * a.d.columns + begin + active * kDepth + c % left_over;
+        if constexpr (SUM) {
+#pragma unroll
+            for (int i = 0; i < NP; ++i) a.out[i * rows * a.d.columns + at] = i == 0 ? a.masked : 0;
+        } else {
+            a.out[party * rows * a.d.columns + at] = party == 0 ? a.masked : 0;
         }
     }
 }
 
 // ---- values -----------------------------------------------------------------------------------------------------
-// A workgroup: 16 rows and a few tiles of 16 columns over a range of cached tokens, 64 at a time.  A wave has one column tile and up to three
-// parties (64-bit words), whose diagonals stay in its registers: 4 ND a party of the 256 that two waves a SIMD leave each.  The rows' digits of the next 64
-// tokens are split into the other half of LDS while the matrix cores work on these.  int32 diagonals hold eight pairs and two products of at
-// most 2^14 a token, so a range is at most kMostTokens long (16 x 4096 x 2^14 = 2^30).
-constexpr int kMostTokens = 4096;
-constexpr int kValueWaves = 8, kValueBlock = 64 * kValueWaves;
-constexpr int value_groups(int n, int word_bytes) { return word_bytes == 4 || n <= 3 ? 1 : n <= 6 ? 2 : 4; }      // of parties
-template <int NP, class T> struct ValueShape {
-    static constexpr int groups = value_groups(NP, sizeof(T)), parties = (NP + groups - 1) / groups, tiles = kValueWaves / groups;
-    static constexpr int lds = 2 * (NP + 1) * (int)sizeof(T) * kFrag;
-};
+// A workgroup: 16 rows and WAVES x 16 columns, a tile a wave, over a range of cached tokens, 64 at a time.  The rows' digits of the next 64 tokens are
+// split into the other half of LDS while the matrix cores work on these; a wave has the loads of two slots in flight, over the turns' ends.  Sums as above;
+// eight pairs and two products of at most 2^14 a token and party, so a range is at most kMostTokens long (16 x 8 x 512 x 2^14 = 2^30).
+constexpr int kMostTokens = 512 * SPIN_MAX_PARTIES;        // times parties
 
-template <int NP, class T>
-__global__ __launch_bounds__(kValueBlock) void values_kernel(AttentionArgs<T> a, int range, T *partial)
+// One element of the result whose parties' products sum to z, truncated.
+template <int NP, class T> __device__ inline void finish(const AttentionArgs<T> &a, size_t at, size_t each, T z)
+{
+    Opened<T> c{a.f};
+    c.add(z);
+    T top[NP], msb[NP];
+#pragma unroll
+    for (int i = 0; i < NP; ++i) {
+        c.add(a.C[i * each + at] + a.r[i * each + at]);
+        top[i] = a.r_top[i * each + at];
+        msb[i] = a.r_msb[i * each + at];
+    }
+#pragma unroll
+    for (int i = 0; i < NP; ++i) a.out[i * each + at] = c.truncated(i, top[i], msb[i]);
+}
+
+template <int NP, class T, bool SUM, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, sizeof(T) == 8 || NP > 6 ? 2 : 4) void values_kernel(AttentionArgs<T> a, int range, T *partial)
 {
     using L = Lane<T>;
-    using S = ValueShape<NP, T>;
-    constexpr int ND = L::ND, W = L::W, kStage = (NP + 1) * ND * kFrag;
-    constexpr bool kEarly = NP <= 4;                                    // their loads (8 registers a party) wait in registers during a turn's products
-    typedef T vec __attribute__((ext_vector_type(L::W), aligned(sizeof(T))));
+    constexpr int ND = L::ND, W = L::W, STEPS = SUM ? NP + 1 : 2, kBlock = 64 * WAVES, kStage = (NP + 1) * ND * kFrag;
+    constexpr int kPieces = kTile * kDepth / W, kParts = (kPieces + kBlock - 1) / kBlock;      // of 16 bytes, of the rows' 64 tokens
+    constexpr bool kEarly = NP * kParts <= (sizeof(T) == 8 ? 3 : 1);              // their loads (8 registers a party) wait in registers during a turn's products
+    typedef T vec __attribute__((ext_vector_type(L::W)));
     extern __shared__ __align__(16) char lds[];
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), h = lane / 16;
     const int share = a.heads / a.c.heads, R = share * a.d.nodes, row_tiles = (R + kTile - 1) / kTile, dim = a.c.dim;
-    const int column_blocks = (dim + S::tiles * kTile - 1) / (S::tiles * kTile);
-    int rest = blockIdx.y;
-    const int row0 = rest % row_tiles * kTile;
-    rest /= row_tiles;
-    const int col0 = (rest % column_blocks * S::tiles + wave % S::tiles) * kTile, party0 = wave / S::tiles * S::parties;
-    const int g = rest / column_blocks, b = blockIdx.z;
+    const int b = SUM ? blockIdx.z : blockIdx.z / NP, party = SUM ? 0 : blockIdx.z % NP;
+    int block, row0;
+    place_of(row_tiles, block, row0);
+    const int column_blocks = (dim + WAVES * kTile - 1) / (WAVES * kTile);
+    const int col0 = (blockIdx.y % column_blocks * WAVES + wave) * kTile, g = blockIdx.y / column_blocks;
     const size_t rows = (size_t)a.batch * a.heads * a.d.nodes, first_row = ((size_t)b * a.heads + (size_t)g * share) * a.d.nodes + row0;
     const int context = a.d.context[b];
     const int limit = context < 0 ? 0 : (int)min((long)a.d.columns, (long)context + a.d.nodes);
-    const int begin = blockIdx.x * range, end = min(begin + range, limit);
+    if ((long)block * range >= a.d.columns) return;
+    const int begin = block * range, end = min(begin + range, limit);
 
-    vec x[NP], m[NP];
-    const int my_row = threadIdx.x / (kDepth / W), my_part = threadIdx.x % (kDepth / W);       // this thread's W tokens of the rows' 64
-    const bool my_there = my_row < kTile && row0 + my_row < R;
-    const u64 my_tree = my_there ? tree_row(a.d, b, (row0 + my_row) % a.d.nodes) : 0;
-    auto fetch = [&](int t0) __attribute__((always_inline)) {                                  // P and A
-        const int t = t0 + my_part * W;
-        const size_t from = (first_row + my_row) * a.d.columns + t;
-        if (my_there && t + W <= a.d.columns) {
-#pragma unroll
-            for (int i = 0; i < NP; ++i) {
-                x[i] = *(const vec *)(a.x + i * rows * a.d.columns + from);
-                m[i] = *(const vec *)(a.A + i * rows * a.d.columns + from);
-            }
-        } else {
-#pragma unroll
-            for (int i = 0; i < NP; ++i)
-#pragma unroll
-                for (int e = 0; e < W; ++e) {
-                    const bool one = my_there && t + e < a.d.columns;
-                    x[i][e] = one ? a.x[i * rows * a.d.columns + from + e] : 0;
-                    m[i][e] = one ? a.A[i * rows * a.d.columns + from + e] : 0;
-                }
-        }
+    vec x[kEarly ? kParts : 1][NP], m[kEarly ? kParts : 1][NP];
+    int pages[kEarly ? kParts : 1];
+    auto piece = [&](int k) __attribute__((always_inline)) {
+        int c = threadIdx.x + k * kBlock;
+        if (kParts > 1) asm volatile("" : "+v"(c));        // what follows from two pieces' places is not kept over the products
+        return c;
     };
-    auto stage = [&](int t0, char *to) __attribute__((always_inline)) {                        // their digits, zero where nothing is seen
-        if (my_row >= kTile) return;
-        const int t = t0 + my_part * W, page = page_of(a.c, b, t);                             // a page holds a multiple of W tokens
+    u64 trees[kParts];
+#pragma unroll
+    for (int k = 0; k < kParts; ++k) {
+        const int row = (threadIdx.x + k * kBlock) / (kDepth / W);
+        trees[k] = tree_row(a.d, b, (row < kTile && row0 + row < R ? row0 + row : 0) % a.d.nodes);
+    }
+    // The table's entry for position t, or its last one; looked at when it is needed, a turn later.
+    auto listed = [&](int t) __attribute__((always_inline)) { return a.c.table[(size_t)b * a.c.table_pages + min(t >> a.c.shift, a.c.table_pages - 1)]; };
+    auto fetch = [&](int t0, int k) __attribute__((always_inline)) {                           // P and A of this thread's k-th piece
+        const int c = piece(k), row = c / (kDepth / W), t = t0 + c % (kDepth / W) * W, v = kEarly ? k : 0;
+        const u32 from = (u32)(row < kTile && row0 + row < R ? row : 0) * a.d.columns;
+        pages[v] = listed(t);                              // a page holds a multiple of W tokens
+#pragma unroll
+        for (int i = 0; i < NP; ++i)
+#pragma unroll
+            for (int e = 0; e < W; ++e) {                  // single words: rows may have any length
+                const u32 at = (from + min(t + e, a.d.columns - 1)) * sizeof(T);
+                x[v][i][e] = at_bytes(a.x + (i * rows + first_row) * a.d.columns, at);
+                m[v][i][e] = at_bytes(a.A + (i * rows + first_row) * a.d.columns, at);
+            }
+    };
+    auto stage = [&](int t0, int k, char *to) __attribute__((always_inline)) {                 // their digits, zero where nothing is seen
+        const int c = piece(k), row = c / (kDepth / W), p = c % (kDepth / W), t = t0 + p * W, v = kEarly ? k : 0;
+        if (row >= kTile) return;
+        const bool there = row0 + row < R && (unsigned)pages[v] < (unsigned)a.c.pages && t >> a.c.shift < a.c.table_pages;
+        const u64 tree = trees[k];
         T w[W];
         bool seen[W];
 #pragma unroll
         for (int e = 0; e < W; ++e) {
-            seen[e] = my_there && page >= 0 && t + e < end && sees(my_tree, a.d.nodes, context, t + e);
+            seen[e] = there && t + e < end && sees(tree, a.d.nodes, context, t + e);
             w[e] = 0;
 #pragma unroll
-            for (int i = 0; i < NP; ++i) w[e] += x[i][e] - m[i][e];
+            for (int i = 0; i < NP; ++i) w[e] += x[v][i][e] - m[v][i][e];
             w[e] = seen[e] ? w[e] : 0;
         }
-        put_digits(to, (my_part % 4) * 16 + my_row, my_part / 4 * W, w);
+        put_digits(to, (p % 4) * 16 + row, p / 4 * W, w);
 #pragma unroll
         for (int i = 0; i < NP; ++i) {
 #pragma unroll
-            for (int e = 0; e < W; ++e) w[e] = seen[e] ? m[i][e] : 0;
-            put_digits(to + (i + 1) * (ND * kFrag), (my_part % 4) * 16 + my_row, my_part / 4 * W, w);
+            for (int e = 0; e < W; ++e) w[e] = seen[e] ? m[v][i][e] : 0;
+            put_digits(to + (i + 1) * (ND * kFrag), (p % 4) * 16 + row, p / 4 * W, w);
         }
     };
-    static_assert(kTile * kDepth / W <= kValueBlock, "one piece a thread");
-    v4i acc[S::parties][ND];
+    auto fetch_early = [&](int t0) __attribute__((always_inline)) {
+        if constexpr (kEarly) {
 #pragma unroll
-    for (int i = 0; i < S::parties; ++i)
+            for (int k = 0; k < kParts; ++k) fetch(t0, k);
+        }
+    };
+    auto stage_all = [&](int t0, char *to) __attribute__((always_inline)) {
 #pragma unroll
-        for (int d = 0; d < ND; ++d) acc[i][d] = v4i{0, 0, 0, 0};
-    const u32 column = min(col0 + lane % 16, dim - 1);     // a column past the row's end reads the last one; it is not stored
+        for (int k = 0; k < kParts; ++k) {
+            if (!kEarly) fetch(t0, k);
+            stage(t0, k, to);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    };
+    u32 lane_at[W];                                        // bytes; a column past the row's end reads the last one and is not stored
+#pragma unroll
+    for (int e = 0; e < W; ++e) lane_at[e] = ((h * W + e) * dim + min(col0 + lane % 16, dim - 1)) * sizeof(T);
     const size_t slot = ((size_t)a.c.pages * a.c.heads << a.c.shift) * dim;
+    const T *slots = a.pool + (SUM ? 0 : party * slot);
+    size_t base[L::loads];                                 // of 4 W tokens, which are on one page
+    int next[L::loads];                                    // that page of the next turn
+    auto look_up = [&](int t0) __attribute__((always_inline)) {
+#pragma unroll
+        for (int j = 0; j < L::loads; ++j) next[j] = listed(t0 + j * 4 * W);
+    };
+    auto find = [&](bool wanted, int t0) __attribute__((always_inline)) {                      // the pool's first rows if not, as for scores
+#pragma unroll
+        for (int j = 0; j < L::loads; ++j) {
+            const int t = t0 + j * 4 * W, page = __builtin_amdgcn_readfirstlane(next[j]);
+            const bool there = (unsigned)page < (unsigned)a.c.pages;       // if not, or past the table, some page's rows: they are not seen
+            base[j] = wanted ? row_at(a.c, 0, there ? page : 0, g, t) : 0;
+        }
+    };
+    T raw[2][16];
+    auto load = [&](T (&w)[16], int s) __attribute__((always_inline)) {
+        const T *from = s == 0 ? a.pool : slots + s * slot;
+#pragma unroll
+        for (int j = 0; j < 16; ++j) w[j] = at_bytes(from + base[j / W], lane_at[j % W]);
+    };
+    v4i acc[ND];
+#pragma unroll
+    for (int d = 0; d < ND; ++d) acc[d] = v4i{0, 0, 0, 0};
     if (begin < end) {
-        fetch(begin);
-        stage(begin, lds);
+        fetch_early(begin);
+        if (col0 < dim) {
+            look_up(begin);
+            find(true, begin);
+            load(raw[0], 0);
+            load(raw[1], 1);
+        }
+        stage_all(begin, lds);
     }
     __syncthreads();
-    for (int t0 = begin, turn = 0; t0 < end; t0 += kDepth, turn ^= 1) {
-        if (kEarly && t0 + kDepth < end) fetch(t0 + kDepth);
+    for (int t0 = begin, half = 0; t0 < end; t0 += kDepth, half ^= 1) {
+        const bool more = t0 + kDepth < end;
+        fetch_early(t0 + kDepth);
+        look_up(t0 + kDepth);
         if (col0 < dim) {
-            const T *base[L::loads];                       // of 4 W tokens, which are on one page
+            const char *left = lds + half * kStage + lane * 16;
+            v4i f[ND], right[ND];
 #pragma unroll
-            for (int j = 0; j < L::loads; ++j) {
-                const int page = __builtin_amdgcn_readfirstlane(page_of(a.c, b, t0 + j * 4 * W));
-                base[j] = a.pool + row_at(a.c, 0, max(page, 0), g, page < 0 ? 0 : t0 + j * 4 * W);
-            }
-            T w[16];
-            auto load = [&](int s) __attribute__((always_inline)) {
-#pragma unroll
-                for (int j = 0; j < 16; ++j) w[j] = (base[j / W] + s * slot)[(u32)((h * W + j % W) * dim) + column];
-            };
-            const char *left = lds + turn * kStage + lane * 16;
-            v4i f[ND];
-            load(0);
-            split<T>(w, f);
-            load(party0 + 1);
-#pragma unroll
-            for (int i = 0; i < S::parties; ++i) {         // a wave whose parties end before has its last one twice, and stores it once
-                v4i right[ND];
-                split<T>(w, right);
-                __builtin_amdgcn_sched_barrier(0);         // its words' registers are the next slot's loads'
-                if (i + 1 < S::parties) load(min(party0 + i + 2, NP));
+            for (int s = 0; s < STEPS; ++s) {
+                split<T>(raw[s % 2], s == 0 ? f : right);
+                __builtin_amdgcn_sched_barrier(0);         // these registers are the loads' of two steps on
+                if (s + 2 == STEPS) find(more, t0 + kDepth);
+                load(raw[s % 2], s + 2 < STEPS ? s + 2 : s % 2);
                 __builtin_amdgcn_sched_barrier(0);
-                multiply<T>(acc[i], left, right);
-                multiply<T>(acc[i], left + min(party0 + i + 1, NP) * (ND * kFrag), f);
+                if (s > 0) multiply<T>(acc, left, right, left + (SUM ? s : party + 1) * (ND * kFrag), f);
             }
         }
-        if (t0 + kDepth < end) {
-            if (!kEarly) fetch(t0 + kDepth);
-            stage(t0 + kDepth, lds + (turn ^ 1) * kStage);
-        }
+        if (more) stage_all(t0 + kDepth, lds + (half ^ 1) * kStage);
         __syncthreads();
     }
     const int col = col0 + lane % 16;
     if (col >= dim) return;
+    const size_t each = rows * dim;
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
         if (row0 + 4 * h + r >= R) continue;
-        const size_t at = (first_row + 4 * h + r) * dim + col, party = rows * dim;
-        T y[S::parties];
-#pragma unroll
-        for (int i = 0; i < S::parties; ++i) y[i] = recombine<T>(acc[i], r);
-        if (S::groups > 1 || partial) {
-#pragma unroll
-            for (int i = 0; i < S::parties; ++i)
-                if (party0 + i < NP) partial[((size_t)blockIdx.x * NP + party0 + i) * party + at] = y[i];
-            continue;
-        }
-        if constexpr (S::groups == 1) {
-            T tr[NP], t_top[NP], t_msb[NP];
-#pragma unroll
-            for (int i = 0; i < NP; ++i) {
-                y[i] += a.C[i * party + at];
-                if (a.f) tr[i] = a.r[i * party + at], t_top[i] = a.r_top[i * party + at], t_msb[i] = a.r_msb[i * party + at];
-            }
-            if (a.f) truncate_shares<NP, T>(y, tr, t_top, t_msb, a.f);
-#pragma unroll
-            for (int i = 0; i < NP; ++i) a.out[i * party + at] = y[i];
-        }
+        const size_t at = (first_row + 4 * h + r) * dim + col;
+        const T z = recombine<T>(acc, r);
+        if (partial) partial[((size_t)block * (SUM ? 1 : NP) + party) * each + at] = z;
+        else if constexpr (SUM) finish<NP, T>(a, at, each, z);
+        else a.out[party * each + at] = a.C[party * each + at] + z;
     }
 }
 
-// Adds the ranges' parts onto C and truncates.
-constexpr int kJoinBlock = 256;
-template <int NP, class T> __global__ __launch_bounds__(kJoinBlock) void join_kernel(AttentionArgs<T> a, int ranges, const T *partial)
+// Adds the ranges' parts: kJoinRows threads an element (of one party where SUM is false), each every kJoinRows-th range.
+constexpr int kJoinRows = 8, kJoinBlock = 256;
+template <int NP, class T, bool SUM> __global__ __launch_bounds__(kJoinBlock) void join_kernel(AttentionArgs<T> a, int ranges, const T *partial)
 {
-    const size_t party = (size_t)a.batch * a.heads * a.d.nodes * a.c.dim, at = (size_t)blockIdx.x * kJoinBlock + threadIdx.x;
-    if (at >= party) return;
-    T y[NP], tr[NP], t_top[NP], t_msb[NP];
-#pragma unroll
-    for (int i = 0; i < NP; ++i) {
-        y[i] = a.C[i * party + at];
-        if (a.f) tr[i] = a.r[i * party + at], t_top[i] = a.r_top[i * party + at], t_msb[i] = a.r_msb[i * party + at];
+    __shared__ T sums[kJoinBlock];
+    const size_t each = (size_t)a.batch * a.heads * a.d.nodes * a.c.dim, count = SUM ? each : NP * each;
+    constexpr int kElements = kJoinBlock / kJoinRows;
+    const size_t at = (size_t)blockIdx.x * kElements + threadIdx.x % kElements;
+    T z = 0;
+    if (at < count) {
+#pragma unroll 4
+        for (int p = threadIdx.x / kElements; p < ranges; p += kJoinRows) z += partial[p * count + at];
     }
-    for (int p = 0; p < ranges; ++p)
+    sums[threadIdx.x] = z;
+    __syncthreads();
+    if (threadIdx.x >= kElements || at >= count) return;
 #pragma unroll
-        for (int i = 0; i < NP; ++i) y[i] += partial[((size_t)p * NP + i) * party + at];
-    if (a.f) truncate_shares<NP, T>(y, tr, t_top, t_msb, a.f);
-#pragma unroll
-    for (int i = 0; i < NP; ++i) a.out[i * party + at] = y[i];
+    for (int k = 1; k < kJoinRows; ++k) z += sums[threadIdx.x + k * kElements];
+    if constexpr (SUM) finish<NP, T>(a, at, each, z);
+    else a.out[at] = a.C[at] + z;
 }
 
-int value_range(int n, int batch, int heads, int cached_heads, int nodes, int columns, int dim, int word_bytes)
+inline int value_waves(int dim) { return dim <= 4 * kTile ? 4 : 8; }
+
+int value_range(int n, int batch, int heads, int cached_heads, int nodes, int columns, int dim)
 {
-    const int width = kValueWaves / value_groups(n, word_bytes) * kTile;
+    const int width = value_waves(dim) * kTile;
     const long groups = (long)batch * cached_heads * ((heads / cached_heads * nodes + kTile - 1) / kTile) * ((dim + width - 1) / width);
-    const long wanted = 1024;                              // workgroups
-    const long ranges = (wanted + groups - 1) / groups;
+    const long wanted = 16384 / value_waves(dim);          // workgroups
+    const long ranges = (wanted + groups - 1) / groups, least = 256, most = kMostTokens / n / kDepth * kDepth;
     const long range = ((columns + ranges - 1) / ranges + kDepth - 1) / kDepth * kDepth;
-    return (int)(range > kMostTokens ? kMostTokens : range);
+    return (int)(range > most ? most : range < least ? least : range);
 }
-inline bool value_parts(int n, int ranges, int word_bytes) { return ranges > 1 || value_groups(n, word_bytes) > 1; }
 
 }  // namespace
 
 size_t cache_values_workspace(int n, int batch, int heads, int cached_heads, int nodes, int columns, int dim, int word_bytes)
 {
-    const int range = value_range(n, batch, heads, cached_heads, nodes, columns, dim, word_bytes);
+    const int range = value_range(n, batch, heads, cached_heads, nodes, columns, dim);
     const size_t ranges = ((size_t)columns + range - 1) / range;
-    return 256 + (value_parts(n, (int)ranges, word_bytes) ? ranges * n * batch * heads * nodes * dim * word_bytes : 0);
+    return 256 + (ranges > 1 ? ranges * n * batch * heads * nodes * dim * word_bytes : 0);
 }
 
 template <class T> spin_status launch_cache_scores(const AttentionArgs<T> &a, hipStream_t s)
@@ -451,11 +540,17 @@ template <class T> spin_status launch_cache_scores(const AttentionArgs<T> &a, hi
         const long blocks = ((long)a.d.columns + kDepth - 1) / kDepth, groups = (long)row_tiles * a.c.heads * a.batch;
         long runs = blocks * groups / 1024;
         runs = runs < 1 ? 1 : runs > 16 ? 16 : runs;
-        static OncePerDevice lds_flags;
-        st = allow_dynamic_lds((const void *)scores_kernel<NP, T>, kMostLds, lds_flags);
-        if (st != SPIN_OK) return;
-        const dim3 grid((unsigned)((blocks + runs - 1) / runs), row_tiles * a.c.heads, a.batch);
-        scores_kernel<NP, T><<<grid, kScoreBlock, held * kSlots, s>>>(a, (int)runs, held);
+        const long strips = ((blocks + runs - 1) / runs + kXcds - 1) / kXcds;
+        auto go = [&](auto sum) {
+            constexpr bool SUM = decltype(sum)::value;
+            static OncePerDevice lds_flags;
+            st = allow_dynamic_lds((const void *)scores_kernel<NP, T, SUM>, kMostLds, lds_flags);
+            if (st != SPIN_OK) return;
+            const dim3 grid((unsigned)(strips * kXcds * row_tiles), a.c.heads, SUM ? a.batch : a.batch * NP);
+            scores_kernel<NP, T, SUM><<<grid, kScoreBlock, held * kSlots, s>>>(a, (int)runs, held);
+        };
+        if (a.f) go(std::true_type());
+        else go(std::false_type());
     });
     return st != SPIN_OK ? st : check_launch("spin_cache_scores");
 }
@@ -464,21 +559,30 @@ template <class T> spin_status launch_cache_values(const AttentionArgs<T> &a, hi
 {
     KernelTimer timer(SPIN_KERNEL_ATTENTION, s);
     const int R = a.heads / a.c.heads * a.d.nodes, row_tiles = (R + kTile - 1) / kTile;
-    const int range = value_range(a.n, a.batch, a.heads, a.c.heads, a.d.nodes, a.d.columns, a.c.dim, sizeof(T));
-    const int ranges = (a.d.columns - 1) / range + 1;
-    T *partial = value_parts(a.n, ranges, sizeof(T)) ? (T *)a.workspace : nullptr;
+    const int range = value_range(a.n, a.batch, a.heads, a.c.heads, a.d.nodes, a.d.columns, a.c.dim);
+    const int ranges = (a.d.columns - 1) / range + 1, strips = (ranges + kXcds - 1) / kXcds;
+    T *partial = ranges > 1 ? (T *)a.workspace : nullptr;
     spin_status st = SPIN_OK;
     for_party_count(a.n, [&](auto np) {
-        constexpr int NP = decltype(np)::value;
-        using S = ValueShape<NP, T>;
-        static OncePerDevice lds_flags;
-        st = allow_dynamic_lds((const void *)values_kernel<NP, T>, S::lds, lds_flags);
-        if (st != SPIN_OK) return;
-        const dim3 grid(ranges, row_tiles * ((a.c.dim + S::tiles * kTile - 1) / (S::tiles * kTile)) * a.c.heads, a.batch);
-        values_kernel<NP, T><<<grid, kValueBlock, S::lds, s>>>(a, range, partial);
-        if (!partial) return;
-        const size_t party = (size_t)a.batch * a.heads * a.d.nodes * a.c.dim;
-        join_kernel<NP, T><<<(unsigned)((party + kJoinBlock - 1) / kJoinBlock), kJoinBlock, 0, s>>>(a, ranges, partial);
+        constexpr int NP = decltype(np)::value, kLds = 2 * (NP + 1) * (int)sizeof(T) * kFrag;
+        auto go = [&](auto sum, auto waves) {
+            constexpr bool SUM = decltype(sum)::value;
+            constexpr int WAVES = decltype(waves)::value;
+            static OncePerDevice lds_flags;
+            st = allow_dynamic_lds((const void *)values_kernel<NP, T, SUM, WAVES>, kLds, lds_flags);
+            if (st != SPIN_OK) return;
+            const dim3 grid(strips * kXcds * row_tiles, (a.c.dim + WAVES * kTile - 1) / (WAVES * kTile) * a.c.heads, SUM ? a.batch : a.batch * NP);
+            values_kernel<NP, T, SUM, WAVES><<<grid, 64 * WAVES, kLds, s>>>(a, range, partial);
+            if (!partial) return;
+            const size_t count = (size_t)a.batch * a.heads * a.d.nodes * a.c.dim * (SUM ? 1 : NP), each = kJoinBlock / kJoinRows;
+            join_kernel<NP, T, SUM><<<(unsigned)((count + each - 1) / each), kJoinBlock, 0, s>>>(a, ranges, partial);
+        };
+        auto with = [&](auto sum) {
+            if (value_waves(a.c.dim) == 4) go(sum, std::integral_constant<int, 4>());
+            else go(sum, std::integral_constant<int, 8>());
+        };
+        if (a.f) with(std::true_type());
+        else with(std::false_type());
     });
     return st != SPIN_OK ? st : check_launch("spin_cache_values");
 }

@@ -9,6 +9,7 @@ struct CacheView {                     // of one pool
     int pages, heads, dim, table_pages, shift;           // page_tokens = 1 << shift
     const int32_t *table;
 };
+constexpr int kMostColumns = 1 << 24;   // of a row of scores
 struct DraftView {                     // who sees what
     int nodes, columns;
     const int32_t *context;

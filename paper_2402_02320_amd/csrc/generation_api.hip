@@ -68,7 +68,7 @@ spin_status check_attention(const spin_cache *c, int heads, int nodes, int colum
     const spin_status st = check_cache(c, true);
     if (st != SPIN_OK) return st;
     if (heads < 1 || heads % c->heads != 0 || nodes < 1 || nodes > SPIN_MAX_NODES || columns < 1) return SPIN_EINVAL;
-    if (columns > (1 << 30) || (long)heads * nodes > kMaxGrid || (double)c->n * c->batch * heads * nodes * columns > kMaxWords) return SPIN_ERANGE;
+    if (columns > kMostColumns || (long)heads * nodes > kMaxGrid || (double)c->n * c->batch * heads * nodes * columns > kMaxWords) return SPIN_ERANGE;
     return SPIN_OK;
 }
 

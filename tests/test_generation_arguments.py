@@ -76,7 +76,7 @@ def test_refusals_of_the_attention(L, pre, most):
     for kw in (dict(heads=0), dict(heads=6), dict(nodes=0), dict(nodes=65), dict(columns=0), dict(f=-1), dict(f=most + 1), dict(context=None),
                dict(context=P + 2), dict(tree=ODD)):
         both(**kw)
-    both(columns=(1 << 30) + 1, bad=ERANGE)
+    both(columns=(1 << 24) + 1, bad=ERANGE)
     both(heads=1 << 16, nodes=1, bad=ERANGE)
     for i in range(7):
         for bad in (None, ODD):
