@@ -122,6 +122,7 @@ template <class T> __device__ inline void put_at_bytes(T *scalar, u32 bytes, T v
 //
 // HBM bounds it (a tile of 16 rows of three parties takes 64 KB of cache and 432 MFMA, a sixth of the time), if enough is in flight: a wave has the loads of
 // two slots in flight, over the ends of k-tiles and runs, and reads all of a score's triple and tuple words at once.
+constexpr int kScoreWanted = 2048;     // workgroups
 constexpr int kScoreWaves = 4, kScoreBlock = 64 * kScoreWaves;
 
 template <int NP, class T, bool SUM>
@@ -131,12 +132,16 @@ __global__ __launch_bounds__(kScoreBlock, sizeof(T) == 8 ? 2 : NP < 6 ? 4 : 3) v
     constexpr int ND = L::ND, W = L::W, STEPS = SUM ? NP + 1 : 2;
     typedef T vec __attribute__((ext_vector_type(L::W)));
     extern __shared__ __align__(16) char lds[];
+    __shared__ u64 row_tree[kTile];                        // of this workgroup's rows: what they see, their places behind the context, their bias far from the keys
+    __shared__ int row_place[kTile];
+    __shared__ T row_far[NP][kTile];
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), h = lane / 16;
     const int b = SUM ? blockIdx.z : blockIdx.z / NP, party = SUM ? 0 : blockIdx.z % NP;
     const int share = a.heads / a.c.heads, R = share * a.d.nodes, row_tiles = (R + kTile - 1) / kTile;
     int block, row0;
     place_of(row_tiles, block, row0);
     const int g = blockIdx.y;
+    auto place = [&](int node) { return a.depth ? a.depth[(size_t)b * a.d.nodes + node] : node; };
     const size_t rows = (size_t)a.batch * a.heads * a.d.nodes, first_row = ((size_t)b * a.heads + (size_t)g * share) * a.d.nodes + row0;
     const int context = a.d.context[b], dim = a.c.dim;
     const int limit = context < 0 ? 0 : (int)min((long)a.d.columns, (long)context + a.d.nodes);
@@ -155,7 +160,7 @@ __global__ __launch_bounds__(kScoreBlock, sizeof(T) == 8 ? 2 : NP < 6 ? 4 : 3) v
                 q[i] = *(const vec *)(a.x + i * rows * dim + from);
                 m[i] = *(const vec *)(a.A + i * rows * dim + from);
             }
-            const int p = part % (kDepth / W), to = (p % 4) * 16 + row, byte = p / 4 * W;
+            const int p = part % (kDepth / W), to = (p % 4) * 16 + (row % 4 * 4 + row / 4), byte = p / 4 * W;    // row 4 r + h in the place 4 h + r
             char *frag = lds + (part / (kDepth / W)) * (ND * kFrag);
             T e[W];
 #pragma unroll
@@ -196,6 +201,15 @@ __global__ __launch_bounds__(kScoreBlock, sizeof(T) == 8 ? 2 : NP < 6 ? 4 : 3) v
         page = __builtin_amdgcn_readfirstlane(page_of(a.c, b, t0));
         return row_at(a.c, 0, max(page, 0), g, t0);
     };
+    if (threadIdx.x < kTile) {
+        const int row = min(row0 + (int)threadIdx.x, R - 1), m = row % a.d.nodes;
+        row_tree[threadIdx.x] = tree_row(a.d, b, m);
+        row_place[threadIdx.x] = place(m);
+        const int bucket = a.bias.table ? bucket_at(a.bias, -a.bias.reach) : -1;
+#pragma unroll
+        for (int i = 0; i < NP; ++i)
+            row_far[i][threadIdx.x] = bucket < 0 ? 0 : ((const T *)a.bias.table)[((size_t)i * a.heads + g * share + row / a.d.nodes) * a.bias.buckets + bucket];
+    }
     const bool whole = held >= k_tiles;
     const int active = begin < limit ? min(runs, (limit - begin + kDepth - 1) / kDepth) : 0;   // runs with something to see
     size_t key = 0;
@@ -203,11 +217,12 @@ __global__ __launch_bounds__(kScoreBlock, sizeof(T) == 8 ? 2 : NP < 6 ? 4 : 3) v
         key = key_of(begin);
         load(raw[0], 0, 0, key);
         load(raw[1], 1, 0, key);
-        if (whole) {
-            stage(0, k_tiles);
-            __syncthreads();
-        }
+        if (whole) stage(0, k_tiles);
     }
+    __syncthreads();
+    int nearest = row_place[0];                            // of the rows' places
+    for (int k = 1; k < kTile; ++k) nearest = min(nearest, row_place[k]);
+    nearest = __builtin_amdgcn_readfirstlane(nearest);
     v4i acc[ND];
 #pragma unroll
     for (int d = 0; d < ND; ++d) acc[d] = v4i{0, 0, 0, 0};
@@ -247,23 +262,31 @@ __global__ __launch_bounds__(kScoreBlock, sizeof(T) == 8 ? 2 : NP < 6 ? 4 : 3) v
         key = next;
         const int t0 = begin + run * kDepth + wave * kTile, t = t0 + lane % 16, near = min(t0, a.d.columns - 1);
         const size_t each = rows * a.d.columns, corner = first_row * a.d.columns + near;
+        // All of the tile is seen; and so far behind all rows that they have one bucket (without a bias, its words are zero).
+        const bool past = t0 + kTile <= context, far = !a.bias.table || (past && (long)t0 + kTile - 1 - context - nearest <= -(long)a.bias.reach);
         ++run;
-        // Rows quarter + r, token t.  What these make of the rows is computed anew for every run: kept over the products it takes 50 registers.
-        int quarter = 4 * h;
+        // Rows 4 r + quarter, token t: few rows are spread over the lanes.  What follows from the rows is computed anew for every run: kept over the products
+        // it takes 50 registers.
+        int quarter = h;
         asm volatile("" : "+v"(quarter));
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
             if (NP > 3) __builtin_amdgcn_sched_barrier(0); // a score's words at a time
-            const int row = row0 + quarter + r, m = row % a.d.nodes;
-            const bool mine = row < R && t < a.d.columns, seen = mine && here >= 0 && sees(tree_row(a.d, b, mine ? m : 0), a.d.nodes, context, t);
-            const u32 at = mine ? ((u32)(quarter + r) * a.d.columns + (t - near)) * sizeof(T) : 0;
+            if (row0 + 4 * r >= R) break;
+            const int row = row0 + 4 * r + quarter;
+            const bool mine = row < R && t < a.d.columns;
+            const bool seen = mine && here >= 0 && (past || sees(row_tree[4 * r + quarter], a.d.nodes, context, t));
+            const u32 at = mine ? ((u32)(4 * r + quarter) * a.d.columns + (t - near)) * sizeof(T) : 0;
             int bucket = -1;
             const T *bias = (const T *)a.bias.table + (size_t)(g * share + row / a.d.nodes) * a.bias.buckets;
-            if (a.bias.table && seen) {
-                auto place = [&](int node) { return a.depth ? a.depth[(size_t)b * a.d.nodes + node] : node; };
-                const long away = (t < context ? (long)t - context : place(t - context)) - (long)place(m);
+            if (a.bias.table && !far && seen) {
+                const long away = (t < context ? (long)t - context : place(t - context)) - (long)row_place[4 * r + quarter];
                 bucket = bucket_at(a.bias, (int)min(max(away, -(long)a.bias.reach), (long)a.bias.reach));
             }
+            // What party i's share gets, of a place that is seen.
+            auto bias_of = [&](int i) __attribute__((always_inline)) {
+                return far ? row_far[i][4 * r + quarter] : bucket < 0 ? 0 : bias[(size_t)i * a.heads * a.bias.buckets + bucket];
+            };
             T z = recombine<T>(acc, r);
             if constexpr (SUM) {
                 Opened<T> c{a.f};
@@ -277,13 +300,11 @@ __global__ __launch_bounds__(kScoreBlock, sizeof(T) == 8 ? 2 : NP < 6 ? 4 : 3) v
                 }
 #pragma unroll
                 for (int i = 0; i < NP; ++i) {
-                    T y = c.truncated(i, top[i], msb[i]);
-                    if (bucket >= 0) y += bias[(size_t)i * a.heads * a.bias.buckets + bucket];
+                    const T y = c.truncated(i, top[i], msb[i]) + bias_of(i);
                     if (mine) put_at_bytes(a.out + (i * each + corner), at, seen ? y : i == 0 ? a.masked : 0);
                 }
             } else if (mine) {
-                z += at_bytes(a.C + (party * each + corner), at);
-                if (bucket >= 0) z += bias[(size_t)party * a.heads * a.bias.buckets + bucket];
+                z += at_bytes(a.C + (party * each + corner), at) + bias_of(party);
                 put_at_bytes(a.out + (party * each + corner), at, seen ? z : party == 0 ? a.masked : 0);
             }
         }
@@ -531,14 +552,14 @@ size_t cache_values_workspace(int n, int batch, int heads, int cached_heads, int
 template <class T> spin_status launch_cache_scores(const AttentionArgs<T> &a, hipStream_t s)
 {
     KernelTimer timer(SPIN_KERNEL_ATTENTION, s);
-    constexpr int kMostLds = 160 << 10;
+    constexpr int kMostLds = 158 << 10;                    // and up to 1.2 KB for what belongs to the rows
     const int R = a.heads / a.c.heads * a.d.nodes, row_tiles = (R + kTile - 1) / kTile, k_tiles = (a.c.dim + kDepth - 1) / kDepth;
     spin_status st = SPIN_OK;
     for_party_count(a.n, [&](auto np) {
         constexpr int NP = decltype(np)::value, kSlots = (NP + 1) * (int)sizeof(T) * kFrag;
         const int held = k_tiles * kSlots <= kMostLds ? k_tiles : 1;
         const long blocks = ((long)a.d.columns + kDepth - 1) / kDepth, groups = (long)row_tiles * a.c.heads * a.batch;
-        long runs = blocks * groups / 1024;
+        long runs = blocks * groups / kScoreWanted;
         runs = runs < 1 ? 1 : runs > 16 ? 16 : runs;
         const long strips = ((blocks + runs - 1) / runs + kXcds - 1) / kXcds;
         auto go = [&](auto sum) {
