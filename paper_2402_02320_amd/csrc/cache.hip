@@ -6,11 +6,33 @@ namespace {
 
 constexpr int kBlock = 256;
 
-template <class T> struct alignas(16) Vec { T e[16 / sizeof(T)]; };
+// Prompts and runs of pages are read and written once: non-temporal accesses from 16 MB on, as in elementwise.hip.
+constexpr size_t kStreamingBytes = (size_t)16 << 20;
+template <class F> inline void for_streaming(size_t bytes, F &&fn)
+{
+    if (bytes >= kStreamingBytes) fn(std::true_type());
+    else fn(std::false_type());
+}
+template <class T> union Vec {         // 16 bytes
+    u32x4 all;
+    T e[16 / sizeof(T)];
+};
+template <bool NT, class T> __device__ inline Vec<T> ld(const T *p)
+{
+    Vec<T> v;
+    v.all = NT ? __builtin_nontemporal_load((const u32x4 *)p) : *(const u32x4 *)p;
+    return v;
+}
+template <bool NT, class T> __device__ inline void st(T *p, Vec<T> v)
+{
+    if (NT) __builtin_nontemporal_store(v.all, (u32x4 *)p);
+    else *(u32x4 *)p = v.all;
+}
 
 // One thread: 16 bytes of one new row, all slots.  F = sum (x_i - b_i) stays in registers; a row moves 2n words an element in and n + 1
-// out, each once.  blockIdx.y = sequence and head, blockIdx.z = K or V.
-template <int NP, class T> __global__ __launch_bounds__(kBlock) void append_kernel(AppendArgs<T> a)
+// out, each once: HBM bounds it (two parties' 4 x 8 heads x 2048 x 128, ragged: 153 us, 5.3 TB/s; 161 with ordinary accesses).
+// blockIdx.y = sequence and head, blockIdx.z = K or V.
+template <int NP, class T, bool NT> __global__ __launch_bounds__(kBlock) void append_kernel(AppendArgs<T> a)
 {
     constexpr int VEC = 16 / sizeof(T);
     const unsigned per_row = a.c.dim / VEC;
@@ -28,8 +50,8 @@ template <int NP, class T> __global__ __launch_bounds__(kBlock) void append_kern
     Vec<T> xv[NP], mv[NP], f;
 #pragma unroll
     for (int i = 0; i < NP; ++i) {
-        xv[i] = *(const Vec<T> *)(x + i * party + from);
-        mv[i] = *(const Vec<T> *)(m + i * party + from);
+        xv[i] = ld<NT>(x + i * party + from);
+        mv[i] = ld<NT>(m + i * party + from);
     }
 #pragma unroll
     for (int k = 0; k < VEC; ++k) {
@@ -40,29 +62,25 @@ template <int NP, class T> __global__ __launch_bounds__(kBlock) void append_kern
     }
     T *to = a.pool[blockIdx.z] + row_at(a.c, 0, page, g, pos) + at;
     const size_t slot = ((size_t)a.c.pages * a.c.heads << a.c.shift) * a.c.dim;
-    *(Vec<T> *)to = f;
+    st<NT>(to, f);
 #pragma unroll
-    for (int i = 0; i < NP; ++i) *(Vec<T> *)(to + (i + 1) * slot) = mv[i];
+    for (int i = 0; i < NP; ++i) st<NT>(to + (i + 1) * slot, mv[i]);
 }
 
-// A page of one slot is contiguous over its heads.  blockIdx.y = pair, blockIdx.z = slot and pool; a thread moves kCopy vectors a block apart.
-constexpr int kCopy = 4;
-template <class T>
+// A page of one slot is contiguous over its heads; a thread moves 16 bytes (48 pages of three parties, 2 x 4 MB each: 70 us, 5.7 TB/s; with four or eight
+// a thread 74 and 77, with ordinary accesses 80).  blockIdx.y = pair, blockIdx.z = slot and pool.
+template <class T, bool NT>
 __global__ __launch_bounds__(kBlock) void copy_kernel(CacheView c, const int32_t *src, const int32_t *dst, T *K, T *V)
 {
     const int from = src[blockIdx.y], to = dst[blockIdx.y];
     if ((unsigned)from >= (unsigned)c.pages || (unsigned)to >= (unsigned)c.pages) return;
-    const size_t words = ((size_t)c.heads << c.shift) * c.dim, vecs = words / (16 / sizeof(T));
+    constexpr int W = 16 / sizeof(T);
+    const size_t words = ((size_t)c.heads << c.shift) * c.dim, vecs = words / W;
     T *pool = (blockIdx.z & 1 ? V : K) + (blockIdx.z >> 1) * words * c.pages;
-    const Vec<T> *in = (const Vec<T> *)(pool + from * words);
-    Vec<T> *out = (Vec<T> *)(pool + to * words), v[kCopy];
-    const size_t first = (size_t)blockIdx.x * (kBlock * kCopy) + threadIdx.x;
-#pragma unroll
-    for (int k = 0; k < kCopy; ++k)
-        if (first + k * kBlock < vecs) v[k] = in[first + k * kBlock];
-#pragma unroll
-    for (int k = 0; k < kCopy; ++k)
-        if (first + k * kBlock < vecs) out[first + k * kBlock] = v[k];
+    const T *in = pool + from * words;
+    T *out = pool + to * words;
+    const size_t v = (size_t)blockIdx.x * kBlock + threadIdx.x;
+    if (v < vecs) st<NT>(out + v * W, ld<NT>(in + v * W));
 }
 
 // One thread: 16 bytes of one head and slot of all kept rows, kAhead rows read before the first of them is written.  kept ascends, so a row
@@ -100,7 +118,10 @@ template <class T> spin_status launch_cache_append(const AppendArgs<T> &a, hipSt
     KernelTimer timer(SPIN_KERNEL_CACHE, s);
     const size_t vecs = (size_t)a.rows * a.c.dim / (16 / sizeof(T));
     const dim3 grid((unsigned)((vecs + kBlock - 1) / kBlock), a.batch * a.c.heads, 2);
-    for_party_count(a.n, [&](auto np) { append_kernel<decltype(np)::value, T><<<grid, kBlock, 0, s>>>(a); });
+    for_party_count(a.n, [&](auto np) {
+        for_streaming((size_t)a.n * a.batch * a.c.heads * a.rows * a.c.dim * sizeof(T),
+                      [&](auto nt) { append_kernel<decltype(np)::value, T, decltype(nt)::value><<<grid, kBlock, 0, s>>>(a); });
+    });
     return check_launch("spin_cache_append");
 }
 
@@ -108,8 +129,8 @@ template <class T> spin_status launch_cache_copy(const CacheView &c, int n, int 
 {
     KernelTimer timer(SPIN_KERNEL_CACHE, s);
     const size_t vecs = ((size_t)c.heads << c.shift) * c.dim / (16 / sizeof(T));
-    const dim3 grid((unsigned)((vecs + kBlock * kCopy - 1) / (kBlock * kCopy)), pairs, 2 * (n + 1));
-    copy_kernel<T><<<grid, kBlock, 0, s>>>(c, src, dst, K, V);
+    const dim3 grid((unsigned)((vecs + kBlock - 1) / kBlock), pairs, 2 * (n + 1));
+    for_streaming(vecs * 32 * (n + 1) * pairs, [&](auto nt) { copy_kernel<T, decltype(nt)::value><<<grid, kBlock, 0, s>>>(c, src, dst, K, V); });
     return check_launch("spin_cache_copy");
 }
 

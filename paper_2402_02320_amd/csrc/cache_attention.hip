@@ -15,7 +15,6 @@ namespace {
 
 constexpr int kTile = 16;              // query rows, and cached rows (scores) or columns (values), of one MFMA
 constexpr int kDepth = 64;             // k of one MFMA
-constexpr int kXcds = 8;               // workgroups go to the XCDs in turn
 
 template <class T> struct Lane {
     static constexpr int ND = sizeof(T), W = 16 / sizeof(T), loads = 16 / W;

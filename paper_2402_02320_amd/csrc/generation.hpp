@@ -62,6 +62,16 @@ template <class T> spin_status launch_relbias_grad(const PairArgs<T> &a, hipStre
 
 namespace {
 
+constexpr int kXcds = 8;               // workgroups go to the XCDs in turn
+
+// blockIdx.x, turned on from row to row of the grid so that every XCD meets all of its values: left alone a width that divides into the XCDs gives each of them
+// the same few columns, and where some columns have more work than others (masks, diagonals of different lengths) half of the chip waits.
+__device__ inline int turned_x()
+{
+    const unsigned row = blockIdx.y + blockIdx.z * gridDim.y;
+    return (int)((blockIdx.x + row * gridDim.x / kXcds) % gridDim.x);
+}
+
 // The page of position `pos` of sequence b, or -1 where there is none.  pos may be anything.
 __host__ __device__ inline int page_of(const CacheView &c, int b, long pos)
 {
