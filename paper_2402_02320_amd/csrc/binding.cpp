@@ -24,6 +24,32 @@
 
 namespace {
 
+// The calls that exist for 64- and 32-bit words.
+template <class T> struct ByWord;
+template <> struct ByWord<uint64_t> {
+    static constexpr at::ScalarType type = at::kLong;
+    static constexpr int bits = 64;
+    decltype(&spin_cache_append) append;
+    decltype(&spin_cache_copy) copy;
+    decltype(&spin_cache_compact) compact;
+    decltype(&spin_cache_scores) scores;
+    decltype(&spin_cache_values) values;
+    decltype(&spin_cache_values_workspace_bytes) values_bytes;
+    decltype(&spin_relbias_trunc) bias;
+    decltype(&spin_relbias_grad) grad;
+};
+template <> struct ByWord<uint32_t> {
+    static constexpr at::ScalarType type = at::kInt;
+    static constexpr int bits = 32;
+    decltype(&spin32_cache_append) append;
+    decltype(&spin32_cache_copy) copy;
+    decltype(&spin32_cache_compact) compact;
+    decltype(&spin32_cache_scores) scores;
+    decltype(&spin32_cache_values) values;
+    decltype(&spin32_cache_values_workspace_bytes) values_bytes;
+    decltype(&spin32_relbias_trunc) bias;
+    decltype(&spin32_relbias_grad) grad;
+};
 struct Library {
     decltype(&spin_share) share, bshare;
     decltype(&spin_open) open, bopen;
@@ -34,7 +60,14 @@ struct Library {
     decltype(&spin_beaver_matmul_grouped) grouped;
     decltype(&spin_beaver_matmul_grouped_workspace_bytes) grouped_bytes;
     decltype(&spin_completed_square_trunc) completed_square;
+    ByWord<uint64_t> wide;
+    ByWord<uint32_t> narrow;
 } lib;
+template <class T> inline const ByWord<T> &by_word()
+{
+    if constexpr (sizeof(T) == 8) return lib.wide;
+    else return lib.narrow;
+}
 constexpr int kEntries = sizeof(Library) / sizeof(void *);
 size_t unasked_bytes;                                    // workspaces up to this size are taken without a look at the device's memory
 
@@ -335,6 +368,259 @@ PyObject *completed_square(PyObject *const *a, Py_ssize_t count)
     });
 }
 
+// ---- a paged cache, attention over it, relative position bias: (word bits, the arguments of the calls in spin.py) -------------
+using Shape = at::IntArrayRef;
+template <class T> inline const at::Tensor *word_tensor(PyObject *o)
+{
+    if (!THPVariable_CheckExact(o)) return nullptr;
+    const at::Tensor &t = THPVariable_Unpack(o);
+    if (!t.defined() || !t.has_storage() || !t.is_cuda() || t.scalar_type() != ByWord<T>::type || !t.is_contiguous()) return nullptr;
+    return &t;
+}
+template <class T> inline const at::Tensor *word_tensor(PyObject *o, Shape shape)
+{
+    const at::Tensor *t = word_tensor<T>(o);
+    return t && t->sizes() == shape ? t : nullptr;
+}
+// A device list of int32_t (as the 32-bit words are); absent lists stay null.
+inline bool list_of(PyObject *o, Shape shape, const int32_t *&to)
+{
+    to = nullptr;
+    if (o == Py_None) return true;
+    const at::Tensor *t = word_tensor<uint32_t>(o, shape);
+    if (t) to = (const int32_t *)t->const_data_ptr();
+    return t != nullptr;
+}
+template <class T> inline T *data(const at::Tensor *t) { return (T *)t->mutable_data_ptr(); }
+inline bool sequence(PyObject *o, Py_ssize_t count) { return (PyTuple_CheckExact(o) || PyList_CheckExact(o)) && PySequence_Fast_GET_SIZE(o) == count; }
+inline bool fits(std::initializer_list<int64_t> sizes)
+{
+    for (int64_t v : sizes)
+        if (v < 1 || v > 0x7fffffff) return false;
+    return true;
+}
+// The cache of K and V (one of them may be null) and, where it is looked at, its table of `batch` sequences.
+template <class T> inline bool cache_of(const at::Tensor *K, const at::Tensor *V, PyObject *table, int64_t batch, spin_cache &c)
+{
+    const at::Tensor *pool = K ? K : V;
+    if (!pool || pool->dim() != 5 || (K && V && K->sizes() != V->sizes())) return false;
+    const Shape s = pool->sizes();
+    if (!fits({s[1], s[2], s[3], s[4]}) || !parties(s[0] - 1)) return false;
+    c = spin_cache{(int)s[0] - 1, (int)s[1], (int)s[2], (int)s[3], (int)s[4], K ? data<T>(K) : nullptr, V ? data<T>(V) : nullptr, (int)batch, 0, nullptr};
+    if (!table) return true;
+    const at::Tensor *t = word_tensor<uint32_t>(table);
+    if (!t || t->dim() != 2 || t->size(0) != batch || !fits({batch, t->size(1)})) return false;
+    c.table_pages = (int)t->size(1);
+    c.table = (const int32_t *)t->const_data_ptr();
+    return true;
+}
+template <class T> inline bool pools_of(PyObject *o, const at::Tensor *&K, const at::Tensor *&V)
+{
+    return sequence(o, 2) && (K = word_tensor<T>(PySequence_Fast_GET_ITEM(o, 0))) && (V = word_tensor<T>(PySequence_Fast_GET_ITEM(o, 1)));
+}
+template <class T> inline bool tuple_of(PyObject *o, int f, Shape shape, const T *(&r)[3])
+{
+    for (int k = 0; k < 3; ++k) r[k] = nullptr;
+    if (f == 0) return true;
+    if (!sequence(o, 3)) return false;
+    for (int k = 0; k < 3; ++k) {
+        const at::Tensor *t = word_tensor<T>(PySequence_Fast_GET_ITEM(o, k), shape);
+        if (!t) return false;
+        r[k] = data<T>(t);
+    }
+    return true;
+}
+inline bool bucketing(PyObject *o, int64_t buckets, spin_relbias &v)
+{
+    const at::Tensor *t = word_tensor<uint32_t>(o);
+    if (!t || t->dim() != 1 || t->numel() % 2 == 0 || !fits({buckets, t->numel()})) return false;
+    v = spin_relbias{(int)buckets, (int)(t->numel() / 2), (const int32_t *)t->const_data_ptr(), nullptr};
+    return true;
+}
+template <class T> inline bool bias_of(PyObject *table, PyObject *bucket_of, int64_t n, int64_t heads, spin_relbias &v)
+{
+    const at::Tensor *t = word_tensor<T>(table);
+    if (!t || t->dim() != 3 || t->size(0) != n || t->size(1) != heads || !bucketing(bucket_of, t->size(2), v)) return false;
+    v.table = data<T>(t);
+    return true;
+}
+// `out` or a fresh tensor of that shape.
+template <class T> struct Result {
+    const at::Tensor *t = nullptr;
+    at::Tensor fresh;
+    bool take(PyObject *out, Shape shape, const at::Tensor &like)
+    {
+        int64_t words = 1;
+        for (int64_t v : shape) words *= v;
+        if (out != Py_None) return (t = word_tensor<T>(out)) && t->numel() >= words;
+        fresh = at::empty(shape, like.options());
+        t = &fresh;
+        return true;
+    }
+};
+inline PyObject *answer(spin_status st, PyObject *result) { return st == SPIN_OK ? Py_NewRef(result) : PyLong_FromLong(st); }
+
+template <class T> PyObject *cache_append(PyObject *const *a)      // pools, table, start, x, b, count
+{
+    const at::Tensor *K, *V, *Kx, *Vx, *Kb, *Vb;
+    spin_cache c;
+    const int32_t *start, *count;
+    if (!pools_of<T>(a[0], K, V) || !pools_of<T>(a[3], Kx, Vx) || !pools_of<T>(a[4], Kb, Vb) || Kx->dim() != 5) return none();
+    const Shape s = Kx->sizes();
+    if (Vx->sizes() != s || Kb->sizes() != s || Vb->sizes() != s || !fits({s[1], s[3]}) || !cache_of<T>(K, V, a[1], s[1], c)) return none();
+    if (c.n != s[0] || c.heads != s[2] || c.dim != s[4] || !list_of(a[2], s.slice(1, 1), start) || !start || !list_of(a[5], s.slice(1, 1), count)) return none();
+    const int rows = (int)s[3];
+    const T *p[4] = {data<T>(Kx), data<T>(Kb), data<T>(Vx), data<T>(Vb)};
+    return answer(unlocked([&](spin_stream q) { return by_word<T>().append(&c, rows, start, count, p[0], p[1], p[2], p[3], q); }), a[0]);
+}
+template <class T> PyObject *cache_copy(PyObject *const *a)        // pools, src, dst
+{
+    const at::Tensor *K, *V, *src = word_tensor<uint32_t>(a[1]);
+    spin_cache c;
+    const int32_t *from, *to;
+    if (!src || src->dim() != 1 || !fits({src->numel()}) || !pools_of<T>(a[0], K, V) || !cache_of<T>(K, V, nullptr, 0, c)) return none();
+    if (!list_of(a[1], src->sizes(), from) || !list_of(a[2], src->sizes(), to) || !to) return none();
+    const int pairs = (int)src->numel();
+    return answer(unlocked([&](spin_stream q) { return by_word<T>().copy(&c, pairs, from, to, q); }), a[0]);
+}
+template <class T> PyObject *cache_compact(PyObject *const *a)     // pools, table, context, kept, kept_count
+{
+    const at::Tensor *K, *V, *kept = word_tensor<uint32_t>(a[3]);
+    spin_cache c;
+    const int32_t *context, *list, *count;
+    if (!kept || kept->dim() != 2 || !fits({kept->size(0), kept->size(1)}) || !pools_of<T>(a[0], K, V) || !cache_of<T>(K, V, a[1], kept->size(0), c)) return none();
+    const Shape b = kept->sizes().slice(0, 1);
+    if (!list_of(a[2], b, context) || !context || !list_of(a[3], kept->sizes(), list) || !list_of(a[4], b, count) || !count) return none();
+    const int nodes = (int)kept->size(1);
+    return answer(unlocked([&](spin_stream q) { return by_word<T>().compact(&c, nodes, context, list, count, q); }), a[0]);
+}
+// What scores and values share: x, A (of `last` words a row), C, tuple, tree.
+template <class T> struct Attention {
+    spin_cache c;
+    const at::Tensor *x, *A, *C;
+    const T *r[3];
+    const uint64_t *tree = nullptr;
+    const int32_t *context;
+    int f;
+    Shape rows;
+    bool take(PyObject *pool, bool keys, PyObject *table, PyObject *ctx, PyObject *px, PyObject *pA, PyObject *pC, PyObject *pf, PyObject *tup, PyObject *ptree)
+    {
+        x = word_tensor<T>(px), C = word_tensor<T>(pC);
+        if (!x || !C || x->dim() != 5 || C->dim() != 5 || !(A = word_tensor<T>(pA, x->sizes())) || !integer(pf, 0, ByWord<T>::bits - 3, f)) return false;
+        rows = x->sizes().slice(0, 4);
+        const at::Tensor *p = word_tensor<T>(pool);
+        if (C->sizes().slice(0, 4) != rows || !fits({rows[1], rows[2], rows[3], x->size(4), C->size(4)}) ||
+            !cache_of<T>(keys ? p : nullptr, keys ? nullptr : p, table, rows[1], c))
+            return false;
+        if (c.n != rows[0] || c.dim != (keys ? x : C)->size(4) || !list_of(ctx, rows.slice(1, 1), context) || !context || !tuple_of<T>(tup, f, C->sizes(), r)) return false;
+        if (ptree == Py_None) return true;
+        const int64_t shape[2] = {rows[1], rows[3]};
+        const at::Tensor *t = word_tensor<uint64_t>(ptree, Shape(shape, 2));
+        if (t) tree = data<uint64_t>(t);
+        return t != nullptr;
+    }
+};
+template <class T> PyObject *cache_scores(PyObject *const *a)      // K, table, context, Q, A, C, f, tuple, tree, masked, bias, depth, out
+{
+    Attention<T> v;
+    Result<T> out;
+    spin_relbias bias;
+    const int32_t *depth = nullptr;
+    uint64_t masked;
+    if (!v.take(a[0], true, a[1], a[2], a[3], a[4], a[5], a[6], a[7], a[8]) || !word(a[9], masked)) return none();
+    const bool biased = a[10] != Py_None;
+    const int64_t nodes[2] = {v.rows[1], v.rows[3]};
+    if (biased && (!sequence(a[10], 2) || !bias_of<T>(PySequence_Fast_GET_ITEM(a[10], 0), PySequence_Fast_GET_ITEM(a[10], 1), v.rows[0], v.rows[2], bias) ||
+                   !list_of(a[11], Shape(nodes, 2), depth)))
+        return none();
+    if (!out.take(a[12], v.C->sizes(), *v.C)) return none();
+    const T *Q = data<T>(v.x), *A = data<T>(v.A), *C = data<T>(v.C);
+    T *to = data<T>(out.t);
+    return run(*out.t, [&](spin_stream q) {
+        return by_word<T>().scores(&v.c, (int)v.rows[2], (int)v.rows[3], (int)v.C->size(4), v.f, v.context, v.tree, Q, A, C, v.r[0], v.r[1], v.r[2], (T)masked,
+                                   biased ? &bias : nullptr, depth, to, q);
+    });
+}
+template <class T> PyObject *cache_values(PyObject *const *a)      // V, table, context, P, A, C, f, tuple, tree, out, workspace
+{
+    Attention<T> v;
+    Result<T> out;
+    if (!v.take(a[0], false, a[1], a[2], a[3], a[4], a[5], a[6], a[7], a[8]) || !out.take(a[9], v.C->sizes(), *v.C)) return none();
+    const int heads = (int)v.rows[2], nodes = (int)v.rows[3], columns = (int)v.x->size(4);
+    const at::Tensor *ws = nullptr;
+    at::Tensor fresh;
+    if (a[10] != Py_None) {
+        if (!(ws = workspace_tensor(a[10]))) return none();
+    } else {
+        const size_t size = by_word<T>().values_bytes(&v.c, heads, nodes, columns);
+        if (size == 0 || size > unasked_bytes) return none();
+        fresh = at::empty({(int64_t)size}, v.x->options().dtype(at::kByte));
+        ws = &fresh;
+    }
+    const T *P = data<T>(v.x), *A = data<T>(v.A), *C = data<T>(v.C);
+    T *to = data<T>(out.t);
+    void *space = ws->mutable_data_ptr();
+    const size_t bytes = (size_t)ws->numel() * ws->element_size();
+    return run(*out.t, [&](spin_stream q) {
+        return by_word<T>().values(&v.c, heads, nodes, columns, v.f, v.context, v.tree, P, A, C, v.r[0], v.r[1], v.r[2], to, space, bytes, q);
+    });
+}
+template <class T> struct Pairs {                          // x [n, batch, heads, Q, K], first, causal, lengths
+    const at::Tensor *x;
+    int d[5], first;
+    const int32_t *lengths;
+    bool take(PyObject *px, PyObject *pfirst, PyObject *causal, PyObject *plengths)
+    {
+        x = word_tensor<T>(px);
+        if (!x || x->dim() != 5 || !PyBool_Check(causal) || !integer(pfirst, -0x7fffffff, 0x7fffffff, first)) return false;
+        const Shape s = x->sizes();
+        if (!parties(s[0]) || !fits({s[1], s[2], s[3], s[4]}) || !list_of(plengths, s.slice(1, 1), lengths)) return false;
+        for (int k = 0; k < 5; ++k) d[k] = (int)s[k];
+        return true;
+    }
+};
+template <class T> PyObject *relbias_trunc(PyObject *const *a)     // x, bias, bucket_of, f, tuple, first, causal, lengths, masked, out
+{
+    Pairs<T> p;
+    Result<T> out;
+    spin_relbias bias;
+    const T *r[3];
+    int f;
+    uint64_t masked;
+    if (!p.take(a[0], a[5], a[6], a[7]) || !integer(a[3], 0, ByWord<T>::bits - 3, f) || !word(a[8], masked) || !bias_of<T>(a[1], a[2], p.d[0], p.d[2], bias) ||
+        !tuple_of<T>(a[4], f, p.x->sizes(), r) || !out.take(a[9], p.x->sizes(), *p.x))
+        return none();
+    const T *x = data<T>(p.x);
+    T *to = data<T>(out.t);
+    const int causal = a[6] == Py_True;
+    return run(*out.t, [&](spin_stream q) {
+        return by_word<T>().bias(p.d[0], p.d[1], p.d[2], p.d[3], p.d[4], p.first, causal, p.lengths, f, x, r[0], r[1], r[2], (T)masked, &bias, to, q);
+    });
+}
+template <class T> PyObject *relbias_grad(PyObject *const *a)      // dS, bucket_of, buckets, first, causal, lengths, out
+{
+    Pairs<T> p;
+    Result<T> out;
+    spin_relbias bias;
+    int buckets;
+    if (!p.take(a[0], a[3], a[4], a[5]) || !integer(a[2], 1, 0x7fffffff, buckets) || !bucketing(a[1], buckets, bias)) return none();
+    const int64_t shape[3] = {p.d[0], p.d[2], buckets};
+    if (!out.take(a[6], Shape(shape, 3), *p.x)) return none();
+    const T *dS = data<T>(p.x);
+    T *to = data<T>(out.t);
+    const int causal = a[4] == Py_True;
+    return run(*out.t, [&](spin_stream q) { return by_word<T>().grad(p.d[0], p.d[1], p.d[2], p.d[3], p.d[4], p.first, causal, p.lengths, dS, &bias, to, q); });
+}
+// The first argument says which words; `count` follow.
+inline PyObject *either(PyObject *const *a, Py_ssize_t got, Py_ssize_t count, PyObject *(*wide)(PyObject *const *), PyObject *(*narrow)(PyObject *const *))
+{
+    return guarded([&]() -> PyObject * {
+        int bits;
+        if (got != count + 1 || !integer(a[0], 32, 64, bits) || (bits != 32 && bits != 64)) return none();
+        return bits == 64 ? wide(a + 1) : narrow(a + 1);
+    });
+}
+
 // ---- module ---------------------------------------------------------------------------------------------------
 // bind(addresses of the library's functions in the order of Library, bytes that need no look at the device's memory)
 PyObject *bind(PyObject *, PyObject *const *a, Py_ssize_t count)
@@ -364,6 +650,13 @@ PyMethodDef methods[] = {{"bind", (PyCFunction)(void *)bind, METH_FASTCALL, null
                          FAST("matmul", matmul(a, count)),
                          FAST("grouped", grouped(a, count)),
                          FAST("completed_square", completed_square(a, count)),
+                         FAST("cache_append", either(a, count, 6, cache_append<uint64_t>, cache_append<uint32_t>)),
+                         FAST("cache_copy", either(a, count, 3, cache_copy<uint64_t>, cache_copy<uint32_t>)),
+                         FAST("cache_compact", either(a, count, 5, cache_compact<uint64_t>, cache_compact<uint32_t>)),
+                         FAST("cache_scores", either(a, count, 13, cache_scores<uint64_t>, cache_scores<uint32_t>)),
+                         FAST("cache_values", either(a, count, 11, cache_values<uint64_t>, cache_values<uint32_t>)),
+                         FAST("relbias_trunc", either(a, count, 10, relbias_trunc<uint64_t>, relbias_trunc<uint32_t>)),
+                         FAST("relbias_grad", either(a, count, 7, relbias_grad<uint64_t>, relbias_grad<uint32_t>)),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -134,7 +134,10 @@ def _load_binding(L):
     entries = ("share", "bshare", "open", "bopen", "beaver_mul", "beaver_and", "trunc", "beaver_matmul", "beaver_matmul_nt",
                "beaver_matmul_preferred_workspace_bytes", "beaver_matmul_grouped", "beaver_matmul_grouped_workspace_bytes",
                "completed_square_trunc")
-    binding.bind(tuple(ctypes.cast(getattr(L, "spin_" + e), ctypes.c_void_p).value for e in entries), _UNASKED_BYTES)
+    entries = ["spin_" + e for e in entries] + [pre + e for pre in ("spin_", "spin32_") for e in
+                                                ("cache_append", "cache_copy", "cache_compact", "cache_scores", "cache_values", "cache_values_workspace_bytes",
+                                                 "relbias_trunc", "relbias_grad")]
+    binding.bind(tuple(ctypes.cast(getattr(L, e), ctypes.c_void_p).value for e in entries), _UNASKED_BYTES)
     _fast = binding
 
 
@@ -771,6 +774,10 @@ class _Word:
         """Opens new rows of keys and values, x = (keys, values), against their masks b = (for keys, for values), all
         [n, batch, heads, rows, dim], and writes them into pools = (K, V), [n + 1, pages, heads, page tokens, dim]: row s of sequence b at
         position start[b] + s, on the page table[b, position // page tokens].  count: rows of every sequence, if not all.  Returns pools."""
+        if _fast is not None:
+            done = _fast.cache_append(self.bits, pools, table, start, x, b, count)
+            if done is not None:
+                return _done(done)
         (K, V), (Kx, Vx), (Kb, Vb) = pools, x, b
         _shapes(Kx.dim() == 5 and all(t.shape == Kx.shape for t in (Vx, Kb, Vb)))
         n, batch, heads, rows, dim = Kx.shape
@@ -782,6 +789,10 @@ class _Word:
 
     def cache_copy(self, pools, src, dst):
         """Copies pages src of both pools to pages dst (no page twice in dst, none in both).  Returns pools."""
+        if _fast is not None:
+            done = _fast.cache_copy(self.bits, pools, src, dst)
+            if done is not None:
+                return _done(done)
         c = _cache(self, pools[0], pools[1], None, 0)
         _check(self.entry("cache_copy")(ctypes.byref(c), src.numel(), _list32(src, "src", None), _list32(dst, "dst", src.numel()), _stream()))
         return pools
@@ -789,6 +800,10 @@ class _Word:
     def cache_compact(self, pools, table, context, kept, kept_count):
         """Keeps kept[b, :kept_count[b]], ascending, of the drafted tokens that stand at position context[b] and on: their rows move together
         to context[b] and on.  kept: [batch, nodes].  Returns pools."""
+        if _fast is not None:
+            done = _fast.cache_compact(self.bits, pools, table, context, kept, kept_count)
+            if done is not None:
+                return _done(done)
         _shapes(kept.dim() == 2)
         batch, nodes = kept.shape
         c = _cache(self, pools[0], pools[1], table, batch)
@@ -810,6 +825,10 @@ class _Word:
         K: pool; Q, A: [n, batch, query heads, nodes, dim]; C, the truncation tuple and the result: [n, batch, query heads, nodes, columns].
         tree[b, m]: bits of the drafted tokens that node m sees (None: those up to itself).  masked: public word where nothing is seen.
         bias: (table [n, query heads, buckets], bucket_of) is added after truncation, distances by depth[b, m] behind the context."""
+        if _fast is not None:
+            done = _fast.cache_scores(self.bits, K, table, context, Q, A, C, f, tuple_, tree, masked, bias, depth, out)
+            if done is not None:
+                return _done(done)
         _shapes(Q.dim() == 5 and A.shape == Q.shape and C.dim() == 5 and C.shape[:4] == Q.shape[:4])
         n, batch, heads, nodes, dim = Q.shape
         c = _cache(self, K, None, table, batch)
@@ -832,6 +851,10 @@ class _Word:
     def cache_values(self, V, table, context, P, A, C, f=0, tuple_=None, tree=None, out=None, workspace=None):
         """Sums of the cached values that the new tokens see, weighted by P.  V: pool; P, A: [n, batch, query heads, nodes, columns];
         C, the truncation tuple and the result: [n, batch, query heads, nodes, dim].  Everything else as for cache_scores."""
+        if _fast is not None:
+            done = _fast.cache_values(self.bits, V, table, context, P, A, C, f, tuple_, tree, out, workspace)
+            if done is not None:
+                return _done(done)
         _shapes(P.dim() == 5 and A.shape == P.shape and C.dim() == 5 and C.shape[:4] == P.shape[:4])
         n, batch, heads, nodes, columns = P.shape
         c = _cache(self, None, V, table, batch)
@@ -852,6 +875,10 @@ class _Word:
     def relbias_trunc(self, x, bias, bucket_of, f=0, tuple_=None, first=0, causal=False, lengths=None, masked=0, out=None):
         """Scores x [n, batch, heads, Q, K] truncated by f bits plus bias[n, heads, buckets] at the bucket of k - (q + first); `masked` where
         k >= lengths[batch] or, if causal, k > q + first."""
+        if _fast is not None:
+            done = _fast.relbias_trunc(self.bits, x, bias, bucket_of, f, tuple_, first, causal, lengths, masked, out)
+            if done is not None:
+                return _done(done)
         _shapes(x.dim() == 5)
         n, batch, heads, Q, K = x.shape
         v = _bias(self, (bias, bucket_of), n, heads)
@@ -864,6 +891,10 @@ class _Word:
 
     def relbias_grad(self, dS, bucket_of, buckets, first=0, causal=False, lengths=None, out=None):
         """Gradient [n, heads, buckets] of the bias of relbias_trunc from that of its result, dS [n, batch, heads, Q, K]."""
+        if _fast is not None:
+            done = _fast.relbias_grad(self.bits, dS, bucket_of, buckets, first, causal, lengths, out)
+            if done is not None:
+                return _done(done)
         _shapes(dS.dim() == 5)
         n, batch, heads, Q, K = dS.shape
         v = _bucketing(bucket_of, buckets)
