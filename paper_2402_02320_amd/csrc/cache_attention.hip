@@ -39,7 +39,7 @@ template <class T> __device__ inline void split(const T (&w)[16], v4i (&p)[sizeo
         }
 }
 
-// The digits of W words, the e-th of them at byte q + e of lane `lane`, into the ND fragments at `frag`.
+// The digits of two or four words, the e-th of them at byte q + e of lane `lane`, into the ND fragments at `frag`.
 __device__ inline void put_digits(char *frag, int lane, int q, const u64 (&w)[2])
 {
     const u64 a = to_digits<u64>(w[0]), b = to_digits<u64>(w[1]);
@@ -54,18 +54,21 @@ __device__ inline void put_digits(char *frag, int lane, int q, const u64 (&w)[2]
         *(uint16_t *)(at + 3 * kFrag) = (uint16_t)(r >> 16);
     }
 }
-__device__ inline void put_digits(char *frag, int lane, int q, const u32 (&w)[4])
+template <class T> __device__ inline void put_digits(char *frag, int lane, int q, const T (&w)[4])
 {
-    u32 v[4];
 #pragma unroll
-    for (int k = 0; k < 4; ++k) v[k] = to_digits<u32>(w[k]);
-    const u32 t0 = __builtin_amdgcn_perm(v[1], v[0], 0x05010400u), t1 = __builtin_amdgcn_perm(v[1], v[0], 0x07030602u);
-    const u32 t2 = __builtin_amdgcn_perm(v[3], v[2], 0x05010400u), t3 = __builtin_amdgcn_perm(v[3], v[2], 0x07030602u);
-    char *at = frag + lane * 16 + q;
-    *(u32 *)(at) = __builtin_amdgcn_perm(t2, t0, 0x05040100u);
-    *(u32 *)(at + kFrag) = __builtin_amdgcn_perm(t2, t0, 0x07060302u);
-    *(u32 *)(at + 2 * kFrag) = __builtin_amdgcn_perm(t3, t1, 0x05040100u);
-    *(u32 *)(at + 3 * kFrag) = __builtin_amdgcn_perm(t3, t1, 0x07060302u);
+    for (int half = 0; half < (int)sizeof(T) / 4; ++half) {
+        u32 v[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) v[k] = (u32)(to_digits<T>(w[k]) >> (32 * half));
+        const u32 t0 = __builtin_amdgcn_perm(v[1], v[0], 0x05010400u), t1 = __builtin_amdgcn_perm(v[1], v[0], 0x07030602u);
+        const u32 t2 = __builtin_amdgcn_perm(v[3], v[2], 0x05010400u), t3 = __builtin_amdgcn_perm(v[3], v[2], 0x07030602u);
+        char *at = frag + 4 * half * kFrag + lane * 16 + q;
+        *(u32 *)(at) = __builtin_amdgcn_perm(t2, t0, 0x05040100u);
+        *(u32 *)(at + kFrag) = __builtin_amdgcn_perm(t2, t0, 0x07060302u);
+        *(u32 *)(at + 2 * kFrag) = __builtin_amdgcn_perm(t3, t1, 0x05040100u);
+        *(u32 *)(at + 3 * kFrag) = __builtin_amdgcn_perm(t3, t1, 0x07060302u);
+    }
 }
 
 // acc += left0 . right0 + left1 . right1 over all digit pairs that count; left: ND fragments in LDS, this lane's 16 bytes of the first.  One fragment is read
@@ -324,9 +327,11 @@ __global__ __launch_bounds__(kScoreBlock, sizeof(T) == 8 ? 2 : NP < 6 ? 4 : 3) v
 }
 
 // ---- values -----------------------------------------------------------------------------------------------------
-// A workgroup: 16 rows and WAVES x 16 columns, a tile a wave, over a range of cached tokens, 64 at a time.  The rows' digits of the next 64 tokens are
-// split into the other half of LDS while the matrix cores work on these; a wave has the loads of two slots in flight, over the turns' ends.  Sums as above;
-// eight pairs and two products of at most 2^14 a token and party, so a range is at most kMostTokens long (16 x 8 x 512 x 2^14 = 2^30).
+// A workgroup: 16 rows and WAVES x 16 columns, a tile a wave, over a range of cached tokens, 64 at a time.  A wave reads its column tile word by word (16 lanes
+// side by side, 128 or 64 bytes), so here a lane's 16 k are the tokens 16 j + 4 h + e, e < 4, whatever the word: four words of a row of P or A are read and their
+// digits written by one thread.  The rows' digits of the next 64 tokens are split into the other half of LDS while the matrix cores work on these; a wave has the loads
+// of two slots in flight, over the turns' ends.  Sums as above; eight pairs and two products of at most 2^14 a token and party, so a range is at
+// most kMostTokens long (16 x 8 x 512 x 2^14 = 2^30).
 constexpr int kMostTokens = 512 * SPIN_MAX_PARTIES;        // times parties
 
 // One element of the result whose parties' products sum to z, truncated.
@@ -348,12 +353,11 @@ template <int NP, class T> __device__ inline void finish(const AttentionArgs<T> 
 template <int NP, class T, bool SUM, int WAVES>
 __global__ __launch_bounds__(64 * WAVES, sizeof(T) == 8 || NP > 6 ? 2 : 4) void values_kernel(AttentionArgs<T> a, int range, T *partial)
 {
-    using L = Lane<T>;
-    constexpr int ND = L::ND, W = L::W, STEPS = SUM ? NP + 1 : 2, kBlock = 64 * WAVES, kStage = (NP + 1) * ND * kFrag;
-    constexpr int kPieces = kTile * kDepth / W, kParts = (kPieces + kBlock - 1) / kBlock;      // of 16 bytes, of the rows' 64 tokens
-    constexpr bool kEarly = NP * kParts <= (sizeof(T) == 8 ? 3 : 1);              // their loads (8 registers a party) wait in registers during a turn's products
-    typedef T vec __attribute__((ext_vector_type(L::W)));
+    constexpr int ND = sizeof(T), STEPS = SUM ? NP + 1 : 2, kStage = (NP + 1) * ND * kFrag;
+    constexpr int kPieces = kTile * kDepth / 4;            // of four tokens of a row
+    static_assert(kPieces == 4 * 64 && WAVES % 4 == 0, "a piece a thread of four waves");
     extern __shared__ __align__(16) char lds[];
+    __shared__ u64 row_tree[kTile];
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), h = lane / 16;
     const int share = a.heads / a.c.heads, R = share * a.d.nodes, row_tiles = (R + kTile - 1) / kTile, dim = a.c.dim;
     const int b = SUM ? blockIdx.z : blockIdx.z / NP, party = SUM ? 0 : blockIdx.z % NP;
@@ -366,87 +370,80 @@ __global__ __launch_bounds__(64 * WAVES, sizeof(T) == 8 || NP > 6 ? 2 : 4) void 
     const int limit = context < 0 ? 0 : (int)min((long)a.d.columns, (long)context + a.d.nodes);
     if ((long)block * range >= a.d.columns) return;
     const int begin = block * range, end = min(begin + range, limit);
+    if (threadIdx.x < kTile) row_tree[threadIdx.x] = tree_row(a.d, b, min(row0 + (int)threadIdx.x, R - 1) % a.d.nodes);
+    __syncthreads();
 
-    vec x[kEarly ? kParts : 1][NP], m[kEarly ? kParts : 1][NP];
-    int pages[kEarly ? kParts : 1];
-    auto piece = [&](int k) __attribute__((always_inline)) {
-        int c = threadIdx.x + k * kBlock;
-        if (kParts > 1) asm volatile("" : "+v"(c));        // what follows from two pieces' places is not kept over the products
-        return c;
-    };
-    u64 trees[kParts];
-#pragma unroll
-    for (int k = 0; k < kParts; ++k) {
-        const int row = (threadIdx.x + k * kBlock) / (kDepth / W);
-        trees[k] = tree_row(a.d, b, (row < kTile && row0 + row < R ? row0 + row : 0) % a.d.nodes);
-    }
-    // The table's entry for position t, or its last one; looked at when it is needed, a turn later.
+    // The table's entry for position t, or its last one.
     auto listed = [&](int t) __attribute__((always_inline)) { return a.c.table[(size_t)b * a.c.table_pages + min(t >> a.c.shift, a.c.table_pages - 1)]; };
-    auto fetch = [&](int t0, int k) __attribute__((always_inline)) {                           // P and A of this thread's k-th piece
-        const int c = piece(k), row = c / (kDepth / W), t = t0 + c % (kDepth / W) * W, v = kEarly ? k : 0;
-        const u32 from = (u32)(row < kTile && row0 + row < R ? row : 0) * a.d.columns;
-        pages[v] = listed(t);                              // a page holds a multiple of W tokens
+    // Digits of E and A_i of this thread's row and four tokens, zero where nothing is seen.  Eight waves share the slots: the first four have E, which takes all
+    // parties' words, and `firsts` of the A_i.
+    constexpr int firsts = WAVES == 4 ? NP : (NP - 1) / 2;
+    auto stage = [&](int t0, char *to) __attribute__((always_inline)) {
+        int c = threadIdx.x % kPieces;
+        asm volatile("" : "+v"(c));                        // what follows from the piece's place is not kept over the products
+        const int row = c / 16, p = c % 16, t = t0 + 4 * p, at = (p % 4) * 16 + (row + 4 * (p % 4)) % 16;
+        const int page = listed(t);                        // a page holds a multiple of four tokens
+        const bool there = row0 + row < R && (unsigned)page < (unsigned)a.c.pages && t >> a.c.shift < a.c.table_pages;
+        const u32 from = (u32)(row0 + row < R ? row : 0) * a.d.columns;
+        const int past = min(t, a.d.columns - 4), over = min(t, a.d.columns - 1) - past;              // read at `past`: rows end anywhere, but have four words
+        auto read = [&](const T *v, T (&w)[4]) __attribute__((always_inline)) {
+            typedef T pair __attribute__((ext_vector_type(sizeof(T) == 8 ? 2 : 4), aligned(sizeof(T))));
+            constexpr int per = sizeof(pair) / sizeof(T);
 #pragma unroll
-        for (int i = 0; i < NP; ++i)
+            for (int k = 0; k < 4 / per; ++k) {
+                const pair u = *(const pair *)((const char *)v + (from + past + k * per) * (u32)sizeof(T));
 #pragma unroll
-            for (int e = 0; e < W; ++e) {                  // single words: rows may have any length
-                const u32 at = (from + min(t + e, a.d.columns - 1)) * sizeof(T);
-                x[v][i][e] = at_bytes(a.x + (i * rows + first_row) * a.d.columns, at);
-                m[v][i][e] = at_bytes(a.A + (i * rows + first_row) * a.d.columns, at);
+                for (int e = 0; e < per; ++e) w[k * per + e] = u[e];
             }
-    };
-    auto stage = [&](int t0, int k, char *to) __attribute__((always_inline)) {                 // their digits, zero where nothing is seen
-        const int c = piece(k), row = c / (kDepth / W), p = c % (kDepth / W), t = t0 + p * W, v = kEarly ? k : 0;
-        if (row >= kTile) return;
-        const bool there = row0 + row < R && (unsigned)pages[v] < (unsigned)a.c.pages && t >> a.c.shift < a.c.table_pages;
-        const u64 tree = trees[k];
-        T w[W];
-        bool seen[W];
+            // the last words of a row are those behind `over` others
+            w[0] = over & 1 ? w[1] : w[0], w[1] = over & 1 ? w[2] : w[1], w[2] = over & 1 ? w[3] : w[2];
+            w[0] = over & 2 ? w[2] : w[0], w[1] = over & 2 ? w[3] : w[1];
+        };
+        bool seen[4];
 #pragma unroll
-        for (int e = 0; e < W; ++e) {
-            seen[e] = there && t + e < end && sees(tree, a.d.nodes, context, t + e);
-            w[e] = 0;
+        for (int e = 0; e < 4; ++e) seen[e] = there && t + e < end && sees(row_tree[row], a.d.nodes, context, t + e);
+        T m[NP][4];
+        auto put = [&](int i) __attribute__((always_inline)) {
 #pragma unroll
-            for (int i = 0; i < NP; ++i) w[e] += x[v][i][e] - m[v][i][e];
-            w[e] = seen[e] ? w[e] : 0;
-        }
-        put_digits(to, (p % 4) * 16 + row, p / 4 * W, w);
+            for (int e = 0; e < 4; ++e) m[i][e] = seen[e] ? m[i][e] : 0;
+            put_digits<T>(to + (i + 1) * (ND * kFrag), at, p / 4 * 4, m[i]);
+        };
+        if (WAVES == 4 || wave < 4) {
+            T x[NP][4], sum[4] = {0, 0, 0, 0};
 #pragma unroll
-        for (int i = 0; i < NP; ++i) {
+            for (int i = 0; i < NP; ++i) {
+                read(a.x + (i * rows + first_row) * a.d.columns, x[i]);
+                read(a.A + (i * rows + first_row) * a.d.columns, m[i]);
+                if (i == 3) __builtin_amdgcn_sched_barrier(0);             // four parties' words at a time
+            }
 #pragma unroll
-            for (int e = 0; e < W; ++e) w[e] = seen[e] ? m[v][i][e] : 0;
-            put_digits(to + (i + 1) * (ND * kFrag), (p % 4) * 16 + row, p / 4 * W, w);
-        }
-    };
-    auto fetch_early = [&](int t0) __attribute__((always_inline)) {
-        if constexpr (kEarly) {
+            for (int i = 0; i < NP; ++i)
 #pragma unroll
-            for (int k = 0; k < kParts; ++k) fetch(t0, k);
-        }
-    };
-    auto stage_all = [&](int t0, char *to) __attribute__((always_inline)) {
+                for (int e = 0; e < 4; ++e) sum[e] += seen[e] ? x[i][e] - m[i][e] : 0;
+            put_digits<T>(to, at, p / 4 * 4, sum);
 #pragma unroll
-        for (int k = 0; k < kParts; ++k) {
-            if (!kEarly) fetch(t0, k);
-            stage(t0, k, to);
-            __builtin_amdgcn_sched_barrier(0);
+            for (int i = 0; i < firsts; ++i) put(i);
+        } else {
+#pragma unroll
+            for (int i = firsts; i < NP; ++i) read(a.A + (i * rows + first_row) * a.d.columns, m[i]);
+#pragma unroll
+            for (int i = firsts; i < NP; ++i) put(i);
         }
     };
-    u32 lane_at[W];                                        // bytes; a column past the row's end reads the last one and is not stored
-#pragma unroll
-    for (int e = 0; e < W; ++e) lane_at[e] = ((h * W + e) * dim + min(col0 + lane % 16, dim - 1)) * sizeof(T);
+    const u32 lane_at = (h * 4 * dim + min(col0 + lane % 16, dim - 1)) * sizeof(T);            // bytes; a column past the row's end reads the last one and is not stored
+    const int lane_left = (h * 16 + (lane % 16 + 4 * h) % 16) * 16;        // rows are turned on by four from h to h, which keeps the staging threads off each other's banks
     const size_t slot = ((size_t)a.c.pages * a.c.heads << a.c.shift) * dim;
     const T *slots = a.pool + (SUM ? 0 : party * slot);
-    size_t base[L::loads];                                 // of 4 W tokens, which are on one page
-    int next[L::loads];                                    // that page of the next turn
+    size_t base[4];                                        // of 16 tokens, which are on one page
+    int next[4];                                           // that page of the next turn
     auto look_up = [&](int t0) __attribute__((always_inline)) {
 #pragma unroll
-        for (int j = 0; j < L::loads; ++j) next[j] = listed(t0 + j * 4 * W);
+        for (int j = 0; j < 4; ++j) next[j] = listed(t0 + j * 16);
     };
     auto find = [&](bool wanted, int t0) __attribute__((always_inline)) {                      // the pool's first rows if not, as for scores
 #pragma unroll
-        for (int j = 0; j < L::loads; ++j) {
-            const int t = t0 + j * 4 * W, page = __builtin_amdgcn_readfirstlane(next[j]);
+        for (int j = 0; j < 4; ++j) {
+            const int t = t0 + j * 16, page = __builtin_amdgcn_readfirstlane(next[j]);
             const bool there = (unsigned)page < (unsigned)a.c.pages;       // if not, or past the table, some page's rows: they are not seen
             base[j] = wanted ? row_at(a.c, 0, there ? page : 0, g, t) : 0;
         }
@@ -455,28 +452,26 @@ __global__ __launch_bounds__(64 * WAVES, sizeof(T) == 8 || NP > 6 ? 2 : 4) void 
     auto load = [&](T (&w)[16], int s) __attribute__((always_inline)) {
         const T *from = s == 0 ? a.pool : slots + s * slot;
 #pragma unroll
-        for (int j = 0; j < 16; ++j) w[j] = at_bytes(from + base[j / W], lane_at[j % W]);
+        for (int j = 0; j < 16; ++j) w[j] = at_bytes(from + (base[j / 4] + j % 4 * dim), lane_at);
     };
     v4i acc[ND];
 #pragma unroll
     for (int d = 0; d < ND; ++d) acc[d] = v4i{0, 0, 0, 0};
     if (begin < end) {
-        fetch_early(begin);
         if (col0 < dim) {
             look_up(begin);
             find(true, begin);
             load(raw[0], 0);
             load(raw[1], 1);
         }
-        stage_all(begin, lds);
+        stage(begin, lds);
     }
     __syncthreads();
     for (int t0 = begin, half = 0; t0 < end; t0 += kDepth, half ^= 1) {
         const bool more = t0 + kDepth < end;
-        fetch_early(t0 + kDepth);
         look_up(t0 + kDepth);
         if (col0 < dim) {
-            const char *left = lds + half * kStage + lane * 16;
+            const char *left = lds + half * kStage + lane_left;
             v4i f[ND], right[ND];
 #pragma unroll
             for (int s = 0; s < STEPS; ++s) {
@@ -488,7 +483,7 @@ __global__ __launch_bounds__(64 * WAVES, sizeof(T) == 8 || NP > 6 ? 2 : 4) void 
                 if (s > 0) multiply<T>(acc, left, right, left + (SUM ? s : party + 1) * (ND * kFrag), f);
             }
         }
-        if (more) stage_all(t0 + kDepth, lds + (half ^ 1) * kStage);
+        if (more) stage(t0 + kDepth, lds + (half ^ 1) * kStage);
         __syncthreads();
     }
     const int col = col0 + lane % 16;
@@ -525,6 +520,43 @@ template <int NP, class T, bool SUM> __global__ __launch_bounds__(kJoinBlock) vo
     for (int k = 1; k < kJoinRows; ++k) z += sums[threadIdx.x + k * kElements];
     if constexpr (SUM) finish<NP, T>(a, at, each, z);
     else a.out[at] = a.C[at] + z;
+}
+
+// A few tokens at most: one thread an element of the result, on the vector unit.  blockIdx.y = head and node, blockIdx.z = sequence.
+constexpr int kFewTokens = 3, kFewBlock = 64;
+template <int NP, class T> __global__ __launch_bounds__(kFewBlock) void few_values_kernel(AttentionArgs<T> a)
+{
+    const int d = blockIdx.x * kFewBlock + threadIdx.x, b = blockIdx.z, h = blockIdx.y / a.d.nodes, m = blockIdx.y % a.d.nodes;
+    if (d >= a.c.dim) return;
+    const size_t rows = (size_t)a.batch * a.heads * a.d.nodes, row = (size_t)b * a.heads * a.d.nodes + blockIdx.y;
+    const size_t slot = ((size_t)a.c.pages * a.c.heads << a.c.shift) * a.c.dim, each = rows * a.c.dim, at = row * a.c.dim + d;
+    const int context = a.d.context[b];
+    const u64 tree = tree_row(a.d, b, m);
+    T z[NP], sum = 0;
+#pragma unroll
+    for (int i = 0; i < NP; ++i) z[i] = 0;
+    for (int t = 0; t < a.d.columns; ++t) {
+        const int page = page_of(a.c, b, t);
+        if (page < 0 || !sees(tree, a.d.nodes, context, t)) continue;
+        const T *value = a.pool + row_at(a.c, 0, page, h / (a.heads / a.c.heads), t) + d;
+        T e = 0, mask[NP];
+        const T f = value[0];
+#pragma unroll
+        for (int i = 0; i < NP; ++i) {
+            mask[i] = a.A[(i * rows + row) * a.d.columns + t];
+            e += a.x[(i * rows + row) * a.d.columns + t] - mask[i];
+        }
+#pragma unroll
+        for (int i = 0; i < NP; ++i) z[i] += e * value[(i + 1) * slot] + mask[i] * f;
+    }
+    if (a.f) {
+#pragma unroll
+        for (int i = 0; i < NP; ++i) sum += z[i];
+        finish<NP, T>(a, at, each, sum);
+    } else {
+#pragma unroll
+        for (int i = 0; i < NP; ++i) a.out[i * each + at] = a.C[i * each + at] + z[i];
+    }
 }
 
 inline int value_waves(int dim) { return dim <= 4 * kTile ? 4 : 8; }
@@ -584,6 +616,11 @@ template <class T> spin_status launch_cache_values(const AttentionArgs<T> &a, hi
     T *partial = ranges > 1 ? (T *)a.workspace : nullptr;
     spin_status st = SPIN_OK;
     for_party_count(a.n, [&](auto np) {
+        if (a.d.columns <= kFewTokens) {
+            const dim3 grid((a.c.dim + kFewBlock - 1) / kFewBlock, a.heads * a.d.nodes, a.batch);
+            few_values_kernel<decltype(np)::value, T><<<grid, kFewBlock, 0, s>>>(a);
+            return;
+        }
         constexpr int NP = decltype(np)::value, kLds = 2 * (NP + 1) * (int)sizeof(T) * kFrag;
         auto go = [&](auto sum, auto waves) {
             constexpr bool SUM = decltype(sum)::value;
