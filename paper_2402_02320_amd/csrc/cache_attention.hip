@@ -152,6 +152,7 @@ __global__ __launch_bounds__(kScoreBlock, sizeof(T) == 8 ? 2 : NP < 6 ? 4 : 3) v
 
     auto stage = [&](int kt0, int count) __attribute__((always_inline)) {                // digits of E and A_i of k-tiles kt0 .. kt0 + count - 1
         const int per_row = count * (kDepth / W);
+#pragma unroll 2
         for (int c = threadIdx.x; c < kTile * per_row; c += kScoreBlock) {
             const int row = c / per_row, part = c % per_row, at = (kt0 * (kDepth / W) + part) * W;
             const bool there = row0 + row < R && at < dim;
@@ -203,23 +204,44 @@ __global__ __launch_bounds__(kScoreBlock, sizeof(T) == 8 ? 2 : NP < 6 ? 4 : 3) v
         page = __builtin_amdgcn_readfirstlane(page_of(a.c, b, t0));
         return row_at(a.c, 0, max(page, 0), g, t0);
     };
-    if (threadIdx.x < kTile) {
-        const int row = min(row0 + (int)threadIdx.x, R - 1), m = row % a.d.nodes;
-        row_tree[threadIdx.x] = tree_row(a.d, b, m);
-        row_place[threadIdx.x] = place(m);
-        const int bucket = a.bias.table ? bucket_at(a.bias, -a.bias.reach) : -1;
-#pragma unroll
-        for (int i = 0; i < NP; ++i)
-            row_far[i][threadIdx.x] = bucket < 0 ? 0 : ((const T *)a.bias.table)[((size_t)i * a.heads + g * share + row / a.d.nodes) * a.bias.buckets + bucket];
-    }
+    // What the first loads need is looked up before the context has come, the first run's words of rows 0 to 3 are under way before the products (up to three parties': 8
+    // registers each), and the rows' own lookups go on behind the digits: a short call is a chain of such waits.
+    const int my_row = min(row0 + (int)threadIdx.x % kTile, R - 1);
+    const u64 my_tree = tree_row(a.d, b, my_row % a.d.nodes);
+    const int my_place = place(my_row % a.d.nodes), my_bucket = a.bias.table ? bucket_at(a.bias, -a.bias.reach) : -1;
     const bool whole = held >= k_tiles;
+    size_t key = key_of(begin);
     const int active = begin < limit ? min(runs, (limit - begin + kDepth - 1) / kDepth) : 0;   // runs with something to see
-    size_t key = 0;
+    const size_t each = rows * a.d.columns;
+    auto near_of = [&](int first) __attribute__((always_inline)) { return min(first + wave * kTile, a.d.columns - 1); };      // a wave's first token, within the row
+    auto word_at = [&](int row, int first) __attribute__((always_inline)) {                    // bytes from there to this lane's word of a row
+        const int t = first + wave * kTile + lane % 16;
+        return row0 + row < R && t < a.d.columns ? ((u32)row * a.d.columns + (t - near_of(first))) * (u32)sizeof(T) : 0;
+    };
+    constexpr bool kPre = SUM && NP <= 3;
+    T pre[4][kPre ? NP : 1];
     if (active) {
-        key = key_of(begin);
         load(raw[0], 0, 0, key);
         load(raw[1], 1, 0, key);
+        if constexpr (kPre) {
+            const size_t corner = first_row * a.d.columns + near_of(begin);
+            const u32 at = word_at(h, begin);
+#pragma unroll
+            for (int i = 0; i < NP; ++i) {
+                pre[0][i] = at_bytes(a.C + (i * each + corner), at);
+                pre[1][i] = at_bytes(a.r + (i * each + corner), at);
+                pre[2][i] = at_bytes(a.r_top + (i * each + corner), at);
+                pre[3][i] = at_bytes(a.r_msb + (i * each + corner), at);
+            }
+        }
         if (whole) stage(0, k_tiles);
+    }
+    if (threadIdx.x < kTile) {
+        row_tree[threadIdx.x] = my_tree;
+        row_place[threadIdx.x] = my_place;
+#pragma unroll
+        for (int i = 0; i < NP; ++i)
+            row_far[i][threadIdx.x] = my_bucket < 0 ? 0 : ((const T *)a.bias.table)[((size_t)i * a.heads + g * share + my_row / a.d.nodes) * a.bias.buckets + my_bucket];
     }
     __syncthreads();
     int nearest = row_place[0];                            // of the rows' places
@@ -262,8 +284,8 @@ __global__ __launch_bounds__(kScoreBlock, sizeof(T) == 8 ? 2 : NP < 6 ? 4 : 3) v
         kt = kt1;
         if (kt) continue;
         key = next;
-        const int t0 = begin + run * kDepth + wave * kTile, t = t0 + lane % 16, near = min(t0, a.d.columns - 1);
-        const size_t each = rows * a.d.columns, corner = first_row * a.d.columns + near;
+        const int first = begin + run * kDepth, t0 = first + wave * kTile, t = t0 + lane % 16;
+        const size_t corner = first_row * a.d.columns + near_of(first);
         // All of the tile is seen; and so far behind all rows that they have one bucket (without a bias, its words are zero).
         const bool past = t0 + kTile <= context, far = !a.bias.table || (past && (long)t0 + kTile - 1 - context - nearest <= -(long)a.bias.reach);
         ++run;
@@ -278,7 +300,7 @@ __global__ __launch_bounds__(kScoreBlock, sizeof(T) == 8 ? 2 : NP < 6 ? 4 : 3) v
             const int row = row0 + 4 * r + quarter;
             const bool mine = row < R && t < a.d.columns;
             const bool seen = mine && here >= 0 && (past || sees(row_tree[4 * r + quarter], a.d.nodes, context, t));
-            const u32 at = mine ? ((u32)(4 * r + quarter) * a.d.columns + (t - near)) * sizeof(T) : 0;
+            const u32 at = word_at(4 * r + quarter, first);
             int bucket = -1;
             const T *bias = (const T *)a.bias.table + (size_t)(g * share + row / a.d.nodes) * a.bias.buckets;
             if (a.bias.table && !far && seen) {
@@ -294,11 +316,20 @@ __global__ __launch_bounds__(kScoreBlock, sizeof(T) == 8 ? 2 : NP < 6 ? 4 : 3) v
                 Opened<T> c{a.f};
                 c.add(z);
                 T top[NP], msb[NP];
+                if (kPre && r == 0 && run == 1) {
 #pragma unroll
-                for (int i = 0; i < NP; ++i) {
-                    c.add(at_bytes(a.C + (i * each + corner), at) + at_bytes(a.r + (i * each + corner), at));
-                    top[i] = at_bytes(a.r_top + (i * each + corner), at);
-                    msb[i] = at_bytes(a.r_msb + (i * each + corner), at);
+                    for (int i = 0; i < NP; ++i) {
+                        const int k = kPre ? i : 0;
+                        c.add(pre[0][k] + pre[1][k]);
+                        top[i] = pre[2][k], msb[i] = pre[3][k];
+                    }
+                } else {
+#pragma unroll
+                    for (int i = 0; i < NP; ++i) {
+                        c.add(at_bytes(a.C + (i * each + corner), at) + at_bytes(a.r + (i * each + corner), at));
+                        top[i] = at_bytes(a.r_top + (i * each + corner), at);
+                        msb[i] = at_bytes(a.r_msb + (i * each + corner), at);
+                    }
                 }
 #pragma unroll
                 for (int i = 0; i < NP; ++i) {
@@ -357,7 +388,6 @@ __global__ __launch_bounds__(64 * WAVES, sizeof(T) == 8 || NP > 6 ? 2 : 4) void 
     constexpr int kPieces = kTile * kDepth / 4;            // of four tokens of a row
     static_assert(kPieces == 4 * 64 && WAVES % 4 == 0, "a piece a thread of four waves");
     extern __shared__ __align__(16) char lds[];
-    __shared__ u64 row_tree[kTile];
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), h = lane / 16;
     const int share = a.heads / a.c.heads, R = share * a.d.nodes, row_tiles = (R + kTile - 1) / kTile, dim = a.c.dim;
     const int b = SUM ? blockIdx.z : blockIdx.z / NP, party = SUM ? 0 : blockIdx.z % NP;
@@ -370,9 +400,7 @@ __global__ __launch_bounds__(64 * WAVES, sizeof(T) == 8 || NP > 6 ? 2 : 4) void 
     const int limit = context < 0 ? 0 : (int)min((long)a.d.columns, (long)context + a.d.nodes);
     if ((long)block * range >= a.d.columns) return;
     const int begin = block * range, end = min(begin + range, limit);
-    if (threadIdx.x < kTile) row_tree[threadIdx.x] = tree_row(a.d, b, min(row0 + (int)threadIdx.x, R - 1) % a.d.nodes);
-    __syncthreads();
-
+    const u64 my_tree = tree_row(a.d, b, min(row0 + (int)threadIdx.x % kPieces / 16, R - 1) % a.d.nodes);
     // The table's entry for position t, or its last one.
     auto listed = [&](int t) __attribute__((always_inline)) { return a.c.table[(size_t)b * a.c.table_pages + min(t >> a.c.shift, a.c.table_pages - 1)]; };
     // Digits of E and A_i of this thread's row and four tokens, zero where nothing is seen.  Eight waves share the slots: the first four have E, which takes all
@@ -401,7 +429,7 @@ __global__ __launch_bounds__(64 * WAVES, sizeof(T) == 8 || NP > 6 ? 2 : 4) void 
         };
         bool seen[4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) seen[e] = there && t + e < end && sees(row_tree[row], a.d.nodes, context, t + e);
+        for (int e = 0; e < 4; ++e) seen[e] = there && t + e < end && sees(my_tree, a.d.nodes, context, t + e);
         T m[NP][4];
         auto put = [&](int i) __attribute__((always_inline)) {
 #pragma unroll
@@ -409,17 +437,22 @@ __global__ __launch_bounds__(64 * WAVES, sizeof(T) == 8 || NP > 6 ? 2 : 4) void 
             put_digits<T>(to + (i + 1) * (ND * kFrag), at, p / 4 * 4, m[i]);
         };
         if (WAVES == 4 || wave < 4) {
-            T x[NP][4], sum[4] = {0, 0, 0, 0};
+            T sum[4] = {0, 0, 0, 0};
 #pragma unroll
-            for (int i = 0; i < NP; ++i) {
-                read(a.x + (i * rows + first_row) * a.d.columns, x[i]);
-                read(a.A + (i * rows + first_row) * a.d.columns, m[i]);
-                if (i == 3) __builtin_amdgcn_sched_barrier(0);             // four parties' words at a time
+            for (int first = 0; first < NP; first += 4) {                  // four parties' words at a time
+                T x[4][4];
+#pragma unroll
+                for (int i = first; i < min(first + 4, NP); ++i) {
+                    read(a.x + (i * rows + first_row) * a.d.columns, x[i - first]);
+                    read(a.A + (i * rows + first_row) * a.d.columns, m[i]);
+                }
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+#pragma unroll
+                    for (int i = first; i < min(first + 4, NP); ++i) sum[e] += seen[e] ? x[i - first][e] - m[i][e] : 0;
+                    if (NP > 4) computed_here(sum[e]);
+                }
             }
-#pragma unroll
-            for (int i = 0; i < NP; ++i)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) sum[e] += seen[e] ? x[i][e] - m[i][e] : 0;
             put_digits<T>(to, at, p / 4 * 4, sum);
 #pragma unroll
             for (int i = 0; i < firsts; ++i) put(i);
@@ -457,9 +490,9 @@ __global__ __launch_bounds__(64 * WAVES, sizeof(T) == 8 || NP > 6 ? 2 : 4) void 
     v4i acc[ND];
 #pragma unroll
     for (int d = 0; d < ND; ++d) acc[d] = v4i{0, 0, 0, 0};
+    look_up(begin);                                        // while the context comes
     if (begin < end) {
         if (col0 < dim) {
-            look_up(begin);
             find(true, begin);
             load(raw[0], 0);
             load(raw[1], 1);
@@ -501,16 +534,16 @@ __global__ __launch_bounds__(64 * WAVES, sizeof(T) == 8 || NP > 6 ? 2 : 4) void 
 }
 
 // Adds the ranges' parts: kJoinRows threads an element (of one party where SUM is false), each every kJoinRows-th range.
-constexpr int kJoinRows = 8, kJoinBlock = 256;
+constexpr int kJoinRows = 4, kJoinBlock = 256;
 template <int NP, class T, bool SUM> __global__ __launch_bounds__(kJoinBlock) void join_kernel(AttentionArgs<T> a, int ranges, const T *partial)
 {
+    constexpr int kElements = kJoinBlock / kJoinRows;
     __shared__ T sums[kJoinBlock];
     const size_t each = (size_t)a.batch * a.heads * a.d.nodes * a.c.dim, count = SUM ? each : NP * each;
-    constexpr int kElements = kJoinBlock / kJoinRows;
     const size_t at = (size_t)blockIdx.x * kElements + threadIdx.x % kElements;
     T z = 0;
     if (at < count) {
-#pragma unroll 4
+#pragma unroll 8
         for (int p = threadIdx.x / kElements; p < ranges; p += kJoinRows) z += partial[p * count + at];
     }
     sums[threadIdx.x] = z;
@@ -561,21 +594,30 @@ template <int NP, class T> __global__ __launch_bounds__(kFewBlock) void few_valu
 
 inline int value_waves(int dim) { return dim <= 4 * kTile ? 4 : 8; }
 
-int value_range(int n, int batch, int heads, int cached_heads, int nodes, int columns, int dim)
+// Tokens a workgroup, by an estimate: the chip holds `slots` workgroups, of each of which a beginning takes 0.7 of a turn, and with sequences of any length the
+// last round of them is half empty on either side.  us by ranges of 1, 2, 4, 8 turns, the chosen one in brackets: 3 parties' 2 x 8 heads of 64 over 701 tokens
+// [13.9] 18.6 28.9 50.2; 4 x 8 heads of 128 over up to 32769 569 471 422 [402] (16: 487); 2 parties' 8 x 8 over up to 4097 138 112 [111] 176, 32-bit
+// words, 8 x 4 heads of 80 and 35 rows over up to 3008 54 [44] 47 46.
+int value_range(int n, int batch, int heads, int cached_heads, int nodes, int columns, int dim, int word_bytes)
 {
-    const int width = value_waves(dim) * kTile;
-    const long groups = (long)batch * cached_heads * ((heads / cached_heads * nodes + kTile - 1) / kTile) * ((dim + width - 1) / width);
-    const long wanted = 16384 / value_waves(dim);          // workgroups
-    const long ranges = (wanted + groups - 1) / groups, least = 256, most = kMostTokens / n / kDepth * kDepth;
-    const long range = ((columns + ranges - 1) / ranges + kDepth - 1) / kDepth * kDepth;
-    return (int)(range > most ? most : range < least ? least : range);
+    const int waves = value_waves(dim), width = waves * kTile;
+    const double groups = (double)batch * cached_heads * ((heads / cached_heads * nodes + kTile - 1) / kTile) * ((dim + width - 1) / width);
+    const double slots = 256.0 * (8 / waves) * (8 / word_bytes);
+    const int turns = (columns + kDepth - 1) / kDepth, most = kMostTokens / n / kDepth;
+    int best = 1;
+    double least = 0;
+    for (int r = 1; r <= most && (r == 1 || r < 2 * turns); r *= 2) {
+        const double time = (groups * ((turns + r - 1) / r) / slots + 1) * (0.7 + r);
+        if (r == 1 || time < least) best = r, least = time;
+    }
+    return best * kDepth;
 }
 
 }  // namespace
 
 size_t cache_values_workspace(int n, int batch, int heads, int cached_heads, int nodes, int columns, int dim, int word_bytes)
 {
-    const int range = value_range(n, batch, heads, cached_heads, nodes, columns, dim);
+    const int range = value_range(n, batch, heads, cached_heads, nodes, columns, dim, word_bytes);
     const size_t ranges = ((size_t)columns + range - 1) / range;
     return 256 + (ranges > 1 ? ranges * n * batch * heads * nodes * dim * word_bytes : 0);
 }
@@ -611,7 +653,7 @@ template <class T> spin_status launch_cache_values(const AttentionArgs<T> &a, hi
 {
     KernelTimer timer(SPIN_KERNEL_ATTENTION, s);
     const int R = a.heads / a.c.heads * a.d.nodes, row_tiles = (R + kTile - 1) / kTile;
-    const int range = value_range(a.n, a.batch, a.heads, a.c.heads, a.d.nodes, a.d.columns, a.c.dim);
+    const int range = value_range(a.n, a.batch, a.heads, a.c.heads, a.d.nodes, a.d.columns, a.c.dim, sizeof(T));
     const int ranges = (a.d.columns - 1) / range + 1, strips = (ranges + kXcds - 1) / kXcds;
     T *partial = ranges > 1 ? (T *)a.workspace : nullptr;
     spin_status st = SPIN_OK;
