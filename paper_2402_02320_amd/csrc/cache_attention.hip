@@ -100,13 +100,13 @@ template <class T> __device__ inline T recombine(const v4i (&acc)[sizeof(T)], in
     return v;
 }
 
-// The run or range of tokens and the first row of a workgroup.  Row tiles of one run are eight workgroup ids apart: on one XCD, next to each other in time, so
+// The run or range of tokens and the first row of a workgroup, which has `rows` of them.  Row groups of one run are eight workgroup ids apart: on one XCD, next to each other in time, so
 // that its L2 serves all but the first.  Which XCD has a run goes round with the head and the sequence: short sequences have the first runs only.
-__device__ inline void place_of(int row_tiles, int &block, int &row0)
+__device__ inline void place_of(int row_groups, int rows, int &block, int &row0)
 {
-    const int strip = blockIdx.x / (kXcds * row_tiles), within = blockIdx.x % (kXcds * row_tiles);
+    const int strip = blockIdx.x / (kXcds * row_groups), within = blockIdx.x % (kXcds * row_groups);
     block = strip * kXcds + (within + blockIdx.y + blockIdx.z * gridDim.y) % kXcds;
-    row0 = within / kXcds * kTile;
+    row0 = within / kXcds * rows;
 }
 
 // A word at a scalar address and a lane's bytes from there (rows have at most kMostColumns words, so 16 of them are within 2^31 bytes): no register a lane but
@@ -141,7 +141,7 @@ __global__ __launch_bounds__(kScoreBlock, sizeof(T) == 8 ? 2 : NP < 6 ? 4 : 3) v
     const int b = SUM ? blockIdx.z : blockIdx.z / NP, party = SUM ? 0 : blockIdx.z % NP;
     const int share = a.heads / a.c.heads, R = share * a.d.nodes, row_tiles = (R + kTile - 1) / kTile;
     int block, row0;
-    place_of(row_tiles, block, row0);
+    place_of(row_tiles, kTile, block, row0);
     const int g = blockIdx.y;
     auto place = [&](int node) { return a.depth ? a.depth[(size_t)b * a.d.nodes + node] : node; };
     const size_t rows = (size_t)a.batch * a.heads * a.d.nodes, first_row = ((size_t)b * a.heads + (size_t)g * share) * a.d.nodes + row0;
@@ -381,18 +381,18 @@ template <int NP, class T> __device__ inline void finish(const AttentionArgs<T> 
     for (int i = 0; i < NP; ++i) a.out[i * each + at] = c.truncated(i, top[i], msb[i]);
 }
 
-template <int NP, class T, bool SUM, int WAVES>
+template <int NP, class T, bool SUM, int WAVES, int TILES>
 __global__ __launch_bounds__(64 * WAVES, sizeof(T) == 8 || NP > 6 ? 2 : 4) void values_kernel(AttentionArgs<T> a, int range, T *partial)
 {
-    constexpr int ND = sizeof(T), STEPS = SUM ? NP + 1 : 2, kStage = (NP + 1) * ND * kFrag;
+    constexpr int ND = sizeof(T), STEPS = SUM ? NP + 1 : 2, kRows = kTile * TILES, kTileBytes = (NP + 1) * ND * kFrag, kStage = TILES * kTileBytes;
     constexpr int kPieces = kTile * kDepth / 4;            // of four tokens of a row
-    static_assert(kPieces == 4 * 64 && WAVES % 4 == 0, "a piece a thread of four waves");
+    static_assert(kPieces == 4 * 64 && WAVES >= 4 * TILES, "a piece a thread of four waves");
     extern __shared__ __align__(16) char lds[];
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), h = lane / 16;
-    const int share = a.heads / a.c.heads, R = share * a.d.nodes, row_tiles = (R + kTile - 1) / kTile, dim = a.c.dim;
+    const int share = a.heads / a.c.heads, R = share * a.d.nodes, row_groups = (R + kRows - 1) / kRows, dim = a.c.dim;
     const int b = SUM ? blockIdx.z : blockIdx.z / NP, party = SUM ? 0 : blockIdx.z % NP;
     int block, row0;
-    place_of(row_tiles, block, row0);
+    place_of(row_groups, kRows, block, row0);
     const int column_blocks = (dim + WAVES * kTile - 1) / (WAVES * kTile);
     const int col0 = (blockIdx.y % column_blocks * WAVES + wave) * kTile, g = blockIdx.y / column_blocks;
     const size_t rows = (size_t)a.batch * a.heads * a.d.nodes, first_row = ((size_t)b * a.heads + (size_t)g * share) * a.d.nodes + row0;
@@ -400,16 +400,18 @@ __global__ __launch_bounds__(64 * WAVES, sizeof(T) == 8 || NP > 6 ? 2 : 4) void 
     const int limit = context < 0 ? 0 : (int)min((long)a.d.columns, (long)context + a.d.nodes);
     if ((long)block * range >= a.d.columns) return;
     const int begin = block * range, end = min(begin + range, limit);
-    const u64 my_tree = tree_row(a.d, b, min(row0 + (int)threadIdx.x % kPieces / 16, R - 1) % a.d.nodes);
+    const int my_tile = TILES > 1 ? wave / 4 : 0;          // whose digits this wave writes
     // The table's entry for position t, or its last one.
     auto listed = [&](int t) __attribute__((always_inline)) { return a.c.table[(size_t)b * a.c.table_pages + min(t >> a.c.shift, a.c.table_pages - 1)]; };
-    // Digits of E and A_i of this thread's row and four tokens, zero where nothing is seen.  Eight waves share the slots: the first four have E, which takes all
-    // parties' words, and `firsts` of the A_i.
-    constexpr int firsts = WAVES == 4 ? NP : (NP - 1) / 2;
+    // Digits of E and A_i of this thread's row and four tokens, zero where nothing is seen.  Eight waves share the tiles, or the slots of the one: the first four
+    // have E, which takes all parties' words, and `firsts` of the A_i.
+    constexpr bool kShared = WAVES > 4 && TILES == 1;
+    constexpr int firsts = kShared ? (NP - 1) / 2 : NP;
     auto stage = [&](int t0, char *to) __attribute__((always_inline)) {
         int c = threadIdx.x % kPieces;
         asm volatile("" : "+v"(c));                        // what follows from the piece's place is not kept over the products
-        const int row = c / 16, p = c % 16, t = t0 + 4 * p, at = (p % 4) * 16 + (row + 4 * (p % 4)) % 16;
+        const int row = my_tile * kTile + c / 16, p = c % 16, t = t0 + 4 * p, at = (p % 4) * 16 + (row + 4 * (p % 4)) % 16;
+        to += my_tile * kTileBytes;
         const int page = listed(t);                        // a page holds a multiple of four tokens
         const bool there = row0 + row < R && (unsigned)page < (unsigned)a.c.pages && t >> a.c.shift < a.c.table_pages;
         const u32 from = (u32)(row0 + row < R ? row : 0) * a.d.columns;
@@ -427,16 +429,18 @@ __global__ __launch_bounds__(64 * WAVES, sizeof(T) == 8 || NP > 6 ? 2 : 4) void 
             w[0] = over & 1 ? w[1] : w[0], w[1] = over & 1 ? w[2] : w[1], w[2] = over & 1 ? w[3] : w[2];
             w[0] = over & 2 ? w[2] : w[0], w[1] = over & 2 ? w[3] : w[1];
         };
+        u64 tree = 0;                                      // looked up where drafted tokens are
+        if (t + 3 >= context) tree = tree_row(a.d, b, (row0 + row < R ? row0 + row : 0) % a.d.nodes);
         bool seen[4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) seen[e] = there && t + e < end && sees(my_tree, a.d.nodes, context, t + e);
+        for (int e = 0; e < 4; ++e) seen[e] = there && t + e < end && sees(tree, a.d.nodes, context, t + e);
         T m[NP][4];
         auto put = [&](int i) __attribute__((always_inline)) {
 #pragma unroll
             for (int e = 0; e < 4; ++e) m[i][e] = seen[e] ? m[i][e] : 0;
             put_digits<T>(to + (i + 1) * (ND * kFrag), at, p / 4 * 4, m[i]);
         };
-        if (WAVES == 4 || wave < 4) {
+        if (!kShared || wave < 4) {
             T sum[4] = {0, 0, 0, 0};
 #pragma unroll
             for (int first = 0; first < NP; first += 4) {                  // four parties' words at a time
@@ -469,14 +473,16 @@ __global__ __launch_bounds__(64 * WAVES, sizeof(T) == 8 || NP > 6 ? 2 : 4) void 
     const T *slots = a.pool + (SUM ? 0 : party * slot);
     size_t base[4];                                        // of 16 tokens, which are on one page
     int next[4];                                           // that page of the next turn
+    // (The table is not written here, so it may be read as constant memory: by scalar loads, into scalar registers.)
+    const auto *table = (const __attribute__((address_space(4))) int32_t *)(uintptr_t)(a.c.table + (size_t)b * a.c.table_pages);
     auto look_up = [&](int t0) __attribute__((always_inline)) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) next[j] = listed(t0 + j * 16);
+        for (int j = 0; j < 4; ++j) next[j] = table[min((t0 + j * 16) >> a.c.shift, a.c.table_pages - 1)];
     };
     auto find = [&](bool wanted, int t0) __attribute__((always_inline)) {                      // the pool's first rows if not, as for scores
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            const int t = t0 + j * 16, page = __builtin_amdgcn_readfirstlane(next[j]);
+            const int t = t0 + j * 16, page = next[j];
             const bool there = (unsigned)page < (unsigned)a.c.pages;       // if not, or past the table, some page's rows: they are not seen
             base[j] = wanted ? row_at(a.c, 0, there ? page : 0, g, t) : 0;
         }
@@ -487,9 +493,11 @@ __global__ __launch_bounds__(64 * WAVES, sizeof(T) == 8 || NP > 6 ? 2 : 4) void 
 #pragma unroll
         for (int j = 0; j < 16; ++j) w[j] = at_bytes(from + (base[j / 4] + j % 4 * dim), lane_at);
     };
-    v4i acc[ND];
+    v4i acc[TILES][ND];
 #pragma unroll
-    for (int d = 0; d < ND; ++d) acc[d] = v4i{0, 0, 0, 0};
+    for (int u = 0; u < TILES; ++u)
+#pragma unroll
+        for (int d = 0; d < ND; ++d) acc[u][d] = v4i{0, 0, 0, 0};
     look_up(begin);                                        // while the context comes
     if (begin < end) {
         if (col0 < dim) {
@@ -513,7 +521,10 @@ __global__ __launch_bounds__(64 * WAVES, sizeof(T) == 8 || NP > 6 ? 2 : 4) void 
                 if (s + 2 == STEPS) find(more, t0 + kDepth);
                 load(raw[s % 2], s + 2 < STEPS ? s + 2 : s % 2);
                 __builtin_amdgcn_sched_barrier(0);
-                if (s > 0) multiply<T>(acc, left, right, left + (SUM ? s : party + 1) * (ND * kFrag), f);
+                if (s == 0) continue;
+#pragma unroll
+                for (int u = 0; u < TILES; ++u)
+                    multiply<T>(acc[u], left + u * kTileBytes, right, left + u * kTileBytes + (SUM ? s : party + 1) * (ND * kFrag), f);
             }
         }
         if (more) stage(t0 + kDepth, lds + (half ^ 1) * kStage);
@@ -523,10 +534,11 @@ __global__ __launch_bounds__(64 * WAVES, sizeof(T) == 8 || NP > 6 ? 2 : 4) void 
     if (col >= dim) return;
     const size_t each = rows * dim;
 #pragma unroll
-    for (int r = 0; r < 4; ++r) {
-        if (row0 + 4 * h + r >= R) continue;
-        const size_t at = (first_row + 4 * h + r) * dim + col;
-        const T z = recombine<T>(acc, r);
+    for (int r = 0; r < 4 * TILES; ++r) {
+        const int row = r / 4 * kTile + 4 * h + r % 4;
+        if (row0 + row >= R) continue;
+        const size_t at = (first_row + row) * dim + col;
+        const T z = recombine<T>(acc[r / 4], r % 4);
         if (partial) partial[((size_t)block * (SUM ? 1 : NP) + party) * each + at] = z;
         else if constexpr (SUM) finish<NP, T>(a, at, each, z);
         else a.out[party * each + at] = a.C[party * each + at] + z;
@@ -593,6 +605,10 @@ template <int NP, class T> __global__ __launch_bounds__(kFewBlock) void few_valu
 }
 
 inline int value_waves(int dim) { return dim <= 4 * kTile ? 4 : 8; }
+// Tiles of 16 rows a workgroup: two where there are more rows than one has, and registers and LDS for it.  2 parties' 16 heads over 4 cached ones, 16 nodes, two
+// sequences of up to 6016: 95 us, 110 by single tiles; 32-bit words, 35 rows of eight sequences: 40 and 44; 20 and 32 rows of 3 parties: 78 and 78, 96 and 96.
+constexpr bool two_value_tiles(int n, int word_bytes) { return n <= (word_bytes == 8 ? 3 : 2); }
+inline int value_tiles(int n, int rows, int dim, int word_bytes) { return rows > kTile && value_waves(dim) == 8 && two_value_tiles(n, word_bytes) ? 2 : 1; }
 
 // Tokens a workgroup, by an estimate: the chip holds `slots` workgroups, of each of which a beginning takes 0.7 of a turn, and with sequences of any length the
 // last round of them is half empty on either side.  us by ranges of 1, 2, 4, 8 turns, the chosen one in brackets: 3 parties' 2 x 8 heads of 64 over 701 tokens
@@ -600,8 +616,8 @@ inline int value_waves(int dim) { return dim <= 4 * kTile ? 4 : 8; }
 // words, 8 x 4 heads of 80 and 35 rows over up to 3008 54 [44] 47 46.
 int value_range(int n, int batch, int heads, int cached_heads, int nodes, int columns, int dim, int word_bytes)
 {
-    const int waves = value_waves(dim), width = waves * kTile;
-    const double groups = (double)batch * cached_heads * ((heads / cached_heads * nodes + kTile - 1) / kTile) * ((dim + width - 1) / width);
+    const int waves = value_waves(dim), width = waves * kTile, rows = kTile * value_tiles(n, heads / cached_heads * nodes, dim, word_bytes);
+    const double groups = (double)batch * cached_heads * ((heads / cached_heads * nodes + rows - 1) / rows) * ((dim + width - 1) / width);
     const double slots = 256.0 * (8 / waves) * (8 / word_bytes);
     const int turns = (columns + kDepth - 1) / kDepth, most = kMostTokens / n / kDepth;
     int best = 1;
@@ -652,33 +668,35 @@ template <class T> spin_status launch_cache_scores(const AttentionArgs<T> &a, hi
 template <class T> spin_status launch_cache_values(const AttentionArgs<T> &a, hipStream_t s)
 {
     KernelTimer timer(SPIN_KERNEL_ATTENTION, s);
-    const int R = a.heads / a.c.heads * a.d.nodes, row_tiles = (R + kTile - 1) / kTile;
-    const int range = value_range(a.n, a.batch, a.heads, a.c.heads, a.d.nodes, a.d.columns, a.c.dim, sizeof(T));
+    const int R = a.heads / a.c.heads * a.d.nodes, range = value_range(a.n, a.batch, a.heads, a.c.heads, a.d.nodes, a.d.columns, a.c.dim, sizeof(T));
     const int ranges = (a.d.columns - 1) / range + 1, strips = (ranges + kXcds - 1) / kXcds;
     T *partial = ranges > 1 ? (T *)a.workspace : nullptr;
     spin_status st = SPIN_OK;
     for_party_count(a.n, [&](auto np) {
+        constexpr int NP = decltype(np)::value;
         if (a.d.columns <= kFewTokens) {
             const dim3 grid((a.c.dim + kFewBlock - 1) / kFewBlock, a.heads * a.d.nodes, a.batch);
-            few_values_kernel<decltype(np)::value, T><<<grid, kFewBlock, 0, s>>>(a);
+            few_values_kernel<NP, T><<<grid, kFewBlock, 0, s>>>(a);
             return;
         }
-        constexpr int NP = decltype(np)::value, kLds = 2 * (NP + 1) * (int)sizeof(T) * kFrag;
-        auto go = [&](auto sum, auto waves) {
+        auto go = [&](auto sum, auto waves, auto tiles) {
             constexpr bool SUM = decltype(sum)::value;
-            constexpr int WAVES = decltype(waves)::value;
+            constexpr int WAVES = decltype(waves)::value, TILES = decltype(tiles)::value, kRows = kTile * TILES, kLds = 2 * TILES * (NP + 1) * (int)sizeof(T) * kFrag;
             static OncePerDevice lds_flags;
-            st = allow_dynamic_lds((const void *)values_kernel<NP, T, SUM, WAVES>, kLds, lds_flags);
+            st = allow_dynamic_lds((const void *)values_kernel<NP, T, SUM, WAVES, TILES>, kLds, lds_flags);
             if (st != SPIN_OK) return;
-            const dim3 grid(strips * kXcds * row_tiles, (a.c.dim + WAVES * kTile - 1) / (WAVES * kTile) * a.c.heads, SUM ? a.batch : a.batch * NP);
-            values_kernel<NP, T, SUM, WAVES><<<grid, 64 * WAVES, kLds, s>>>(a, range, partial);
+            const dim3 grid(strips * kXcds * ((R + kRows - 1) / kRows), (a.c.dim + WAVES * kTile - 1) / (WAVES * kTile) * a.c.heads, SUM ? a.batch : a.batch * NP);
+            values_kernel<NP, T, SUM, WAVES, TILES><<<grid, 64 * WAVES, kLds, s>>>(a, range, partial);
             if (!partial) return;
             const size_t count = (size_t)a.batch * a.heads * a.d.nodes * a.c.dim * (SUM ? 1 : NP), each = kJoinBlock / kJoinRows;
             join_kernel<NP, T, SUM><<<(unsigned)((count + each - 1) / each), kJoinBlock, 0, s>>>(a, ranges, partial);
         };
         auto with = [&](auto sum) {
-            if (value_waves(a.c.dim) == 4) go(sum, std::integral_constant<int, 4>());
-            else go(sum, std::integral_constant<int, 8>());
+            if constexpr (decltype(sum)::value && two_value_tiles(NP, sizeof(T))) {
+                if (value_tiles(NP, R, a.c.dim, sizeof(T)) == 2) return go(sum, std::integral_constant<int, 8>(), std::integral_constant<int, 2>());
+            }
+            if (value_waves(a.c.dim) == 4) go(sum, std::integral_constant<int, 4>(), std::integral_constant<int, 1>());
+            else go(sum, std::integral_constant<int, 8>(), std::integral_constant<int, 1>());
         };
         if (a.f) with(std::true_type());
         else with(std::false_type());
