@@ -111,7 +111,11 @@ __device__ inline void place_of(int row_groups, int rows, int &block, int &row0)
 
 // A word at a scalar address and a lane's bytes from there (rows have at most kMostColumns words, so 16 of them are within 2^31 bytes): no register a lane but
 // those 32 bits goes into addresses.
-template <class T> __device__ inline T at_bytes(const T *scalar, u32 bytes) { return *(const T *)((const char *)scalar + bytes); }
+template <bool NT = false, class T> __device__ inline T at_bytes(const T *scalar, u32 bytes)
+{
+    const T *p = (const T *)((const char *)scalar + bytes);
+    return NT ? __builtin_nontemporal_load(p) : *p;
+}
 template <class T> __device__ inline void put_at_bytes(T *scalar, u32 bytes, T v) { *(T *)((char *)scalar + bytes) = v; }
 
 // ---- scores -----------------------------------------------------------------------------------------------------
@@ -381,7 +385,7 @@ template <int NP, class T> __device__ inline void finish(const AttentionArgs<T> 
     for (int i = 0; i < NP; ++i) a.out[i * each + at] = c.truncated(i, top[i], msb[i]);
 }
 
-template <int NP, class T, bool SUM, int WAVES, int TILES>
+template <int NP, class T, bool SUM, int WAVES, int TILES, bool NT>
 __global__ __launch_bounds__(64 * WAVES, sizeof(T) == 8 || NP > 6 ? 2 : 4) void values_kernel(AttentionArgs<T> a, int range, T *partial)
 {
     constexpr int ND = sizeof(T), STEPS = SUM ? NP + 1 : 2, kRows = kTile * TILES, kTileBytes = (NP + 1) * ND * kFrag, kStage = TILES * kTileBytes;
@@ -491,7 +495,7 @@ __global__ __launch_bounds__(64 * WAVES, sizeof(T) == 8 || NP > 6 ? 2 : 4) void 
     auto load = [&](T (&w)[16], int s) __attribute__((always_inline)) {
         const T *from = s == 0 ? a.pool : slots + s * slot;
 #pragma unroll
-        for (int j = 0; j < 16; ++j) w[j] = at_bytes(from + (base[j / 4] + j % 4 * dim), lane_at);
+        for (int j = 0; j < 16; ++j) w[j] = at_bytes<NT>(from + (base[j / 4] + j % 4 * dim), lane_at);
     };
     v4i acc[TILES][ND];
 #pragma unroll
@@ -605,6 +609,7 @@ template <int NP, class T> __global__ __launch_bounds__(kFewBlock) void few_valu
 }
 
 inline int value_waves(int dim) { return dim <= 4 * kTile ? 4 : 8; }
+constexpr double kKept = 256 << 20;    // bytes of the Infinity Cache
 // Tiles of 16 rows a workgroup: two where there are more rows than one has, and registers and LDS for it.  2 parties' 16 heads over 4 cached ones, 16 nodes, two
 // sequences of up to 6016: 95 us, 110 by single tiles; 32-bit words, 35 rows of eight sequences: 40 and 44; 20 and 32 rows of 3 parties: 78 and 78, 96 and 96.
 constexpr bool two_value_tiles(int n, int word_bytes) { return n <= (word_bytes == 8 ? 3 : 2); }
@@ -671,6 +676,10 @@ template <class T> spin_status launch_cache_values(const AttentionArgs<T> &a, hi
     const int R = a.heads / a.c.heads * a.d.nodes, range = value_range(a.n, a.batch, a.heads, a.c.heads, a.d.nodes, a.d.columns, a.c.dim, sizeof(T));
     const int ranges = (a.d.columns - 1) / range + 1, strips = (ranges + kXcds - 1) / kXcds;
     T *partial = ranges > 1 ? (T *)a.workspace : nullptr;
+    // A cache larger than what the chip keeps, read once: non-temporal loads, where a wave's 16 words are whole cache lines (64-bit words, rows of whole tiles) and no
+    // other row tile reads them.  3 parties' 4 x 8 heads over up to 32769 tokens 382 us, 405 with ordinary loads; 32-bit words, half a line, 231 and 208.
+    const bool streamed = R <= kTile && a.c.dim % kTile == 0 &&
+                          (double)(a.n + 1) * a.batch * a.c.heads * a.d.columns * a.c.dim * sizeof(T) > kKept;
     spin_status st = SPIN_OK;
     for_party_count(a.n, [&](auto np) {
         constexpr int NP = decltype(np)::value;
@@ -679,24 +688,28 @@ template <class T> spin_status launch_cache_values(const AttentionArgs<T> &a, hi
             few_values_kernel<NP, T><<<grid, kFewBlock, 0, s>>>(a);
             return;
         }
-        auto go = [&](auto sum, auto waves, auto tiles) {
-            constexpr bool SUM = decltype(sum)::value;
+        auto go = [&](auto sum, auto waves, auto tiles, auto nt) {
+            constexpr bool SUM = decltype(sum)::value, NT = decltype(nt)::value;
             constexpr int WAVES = decltype(waves)::value, TILES = decltype(tiles)::value, kRows = kTile * TILES, kLds = 2 * TILES * (NP + 1) * (int)sizeof(T) * kFrag;
             static OncePerDevice lds_flags;
-            st = allow_dynamic_lds((const void *)values_kernel<NP, T, SUM, WAVES, TILES>, kLds, lds_flags);
+            st = allow_dynamic_lds((const void *)values_kernel<NP, T, SUM, WAVES, TILES, NT>, kLds, lds_flags);
             if (st != SPIN_OK) return;
             const dim3 grid(strips * kXcds * ((R + kRows - 1) / kRows), (a.c.dim + WAVES * kTile - 1) / (WAVES * kTile) * a.c.heads, SUM ? a.batch : a.batch * NP);
-            values_kernel<NP, T, SUM, WAVES, TILES><<<grid, 64 * WAVES, kLds, s>>>(a, range, partial);
+            values_kernel<NP, T, SUM, WAVES, TILES, NT><<<grid, 64 * WAVES, kLds, s>>>(a, range, partial);
             if (!partial) return;
             const size_t count = (size_t)a.batch * a.heads * a.d.nodes * a.c.dim * (SUM ? 1 : NP), each = kJoinBlock / kJoinRows;
             join_kernel<NP, T, SUM><<<(unsigned)((count + each - 1) / each), kJoinBlock, 0, s>>>(a, ranges, partial);
         };
         auto with = [&](auto sum) {
             if constexpr (decltype(sum)::value && two_value_tiles(NP, sizeof(T))) {
-                if (value_tiles(NP, R, a.c.dim, sizeof(T)) == 2) return go(sum, std::integral_constant<int, 8>(), std::integral_constant<int, 2>());
+                if (value_tiles(NP, R, a.c.dim, sizeof(T)) == 2) return go(sum, std::integral_constant<int, 8>(), std::integral_constant<int, 2>(), std::false_type());
             }
-            if (value_waves(a.c.dim) == 4) go(sum, std::integral_constant<int, 4>(), std::integral_constant<int, 1>());
-            else go(sum, std::integral_constant<int, 8>(), std::integral_constant<int, 1>());
+            const std::integral_constant<int, 1> one;
+            if (value_waves(a.c.dim) == 4) return go(sum, std::integral_constant<int, 4>(), one, std::false_type());
+            if constexpr (decltype(sum)::value && sizeof(T) == 8) {
+                if (streamed) return go(sum, std::integral_constant<int, 8>(), one, std::true_type());
+            }
+            go(sum, std::integral_constant<int, 8>(), one, std::false_type());
         };
         if (a.f) with(std::true_type());
         else with(std::false_type());

@@ -310,3 +310,65 @@ def test_offsets_past_32_bits():
     spin.ring32.cache_copy(pools, ints([pages - 1]), ints([pages - 4]))
     torch.cuda.synchronize()
     assert same(K[:, -4:], small)
+
+
+@BITS
+@pytest.mark.parametrize("n,dim,context", [(8, 256, 130), (3, 128, 700)])
+def test_largest_sums_of_scores(bits, n, dim, context):
+    """Every digit of every factor is -128, so the int32 diagonals are as large as they get; the words have a closed form."""
+    ring, unsigned, _ = RINGS[bits]
+    w = int(-(0x8080808080808080 % (1 << bits))) % (1 << bits)
+    word = dev(np.array([w], unsigned))
+    heads, nodes, columns = 4, 5, context + 5
+    pool = word.expand((n + 1, 1, 1, 1024, dim)).contiguous()
+    A = word.expand((n, 1, heads, nodes, dim)).contiguous()
+    Q = A.clone()
+    Q[0] += word                                              # E = sum (Q - A) = the word
+    C = dev(uniform(np.random.default_rng(n), bits, n, 1, heads, nodes, columns))
+    got = ring.cache_scores(pool, ints([[0]]), ints([context]), Q, A, C, masked=3)
+    seen = torch.arange(columns, device="cuda") <= context + torch.arange(nodes, device="cuda")[:, None]
+    want = torch.where(seen, C + 2 * dim * word * word, 0)
+    want[0] += torch.where(seen, 0, 3).to(C.dtype)
+    assert torch.equal(got, want)
+    tup = [dev(uniform(np.random.default_rng(n + k), bits, *C.shape)) for k in range(3)]
+    got = ring.cache_scores(pool, ints([[0]]), ints([context]), Q, A, C, f=9, tuple_=tup, masked=3)
+    want = torch.where(seen, ring.trunc((C + 2 * dim * word * word).view(n, -1), *[t.view(n, -1) for t in tup], 9).view(C.shape), 0)
+    want[0] += torch.where(seen, 0, 3).to(C.dtype)
+    assert torch.equal(got, want)
+
+
+@BITS
+@pytest.mark.parametrize("n,nodes,dim", [(8, 1, 128), (3, 3, 128), (1, 1, 64)])
+def test_largest_sums_of_values(bits, n, nodes, dim):
+    """The same over the longest ranges that a workgroup sums in int32 (all pages of the table are one page)."""
+    ring, unsigned, _ = RINGS[bits]
+    w = int(-(0x8080808080808080 % (1 << bits))) % (1 << bits)
+    word = dev(np.array([w], unsigned))
+    batch, heads, context = 4, 8, 32768 - nodes
+    pool = word.expand((n + 1, 1, heads, 1024, dim)).contiguous()
+    A = word.expand((n, batch, heads, nodes, context + nodes)).contiguous()
+    P = A.clone()
+    P[0] += word
+    C = dev(uniform(np.random.default_rng(n), bits, n, batch, heads, nodes, dim))
+    table = torch.zeros((batch, 32), dtype=torch.int32, device="cuda")
+    count = (context + 1 + torch.arange(nodes, device="cuda")).to(C.dtype)[:, None]
+    plain = C + 2 * count * word * word
+    assert torch.equal(ring.cache_values(pool, table, ints([context] * batch), P, A, C), plain)
+    tup = [dev(uniform(np.random.default_rng(n + k), bits, *C.shape)) for k in range(3)]
+    got = ring.cache_values(pool, table, ints([context] * batch), P, A, C, f=9, tuple_=tup)
+    assert torch.equal(got, ring.trunc(plain.view(n, -1), *[t.view(n, -1) for t in tup], 9).view(C.shape))
+
+
+@pytest.mark.parametrize("n,heads,dim,context", [(2, 1, 128, 150), (3, 2, 112, 17)])
+def test_values_of_a_wide_call_with_short_contexts(n, heads, dim, context):
+    """Columns for a cache larger than the chip keeps (read with non-temporal loads), most of them past the table."""
+    rng = np.random.default_rng(dim)
+    columns, nodes = (1 << 28) // (8 * (n + 1) * heads * dim) + 77, 2
+    pool, table = uniform(rng, 64, n + 1, 14, heads, 16, dim), table_of(rng, 1, 12, 14)
+    P, A = uniform(rng, 64, n, 1, heads, nodes, columns), uniform(rng, 64, n, 1, heads, nodes, columns)
+    C, tree = uniform(rng, 64, n, 1, heads, nodes, dim), np.array([[1, 3]])
+    tup = tuple_of(rng, 64, C.shape)
+    short = 12 * 16 + 3                                       # nothing beyond the table is seen
+    want = gen.values(pool, table, np.array([context]), P[..., :short], A[..., :short], C, 16, tup, tree)
+    got = spin.cache_values(dev(pool), ints(table), ints([context]), dev(P), dev(A), dev(C), f=16, tuple_=[dev(t) for t in tup], tree=dev(tree))
+    assert same(got, want)
