@@ -30,7 +30,7 @@ template <bool NT, class T> __device__ inline void st(T *p, Vec<T> v)
 }
 
 // One thread: 16 bytes of one new row, all slots.  F = sum (x_i - b_i) stays in registers; a row moves 2n words an element in and n + 1
-// out, each once: HBM bounds it (two parties' 4 x 8 heads x 2048 x 128, ragged: 153 us, 5.3 TB/s; 161 with ordinary accesses).
+// out, each once: HBM bounds it (two parties' 4 x 8 heads x 2048 x 128, ragged: 151 us, 5.3 TB/s; 161 with ordinary accesses).
 // blockIdx.y = sequence and head, blockIdx.z = K or V.
 template <int NP, class T, bool NT> __global__ __launch_bounds__(kBlock) void append_kernel(AppendArgs<T> a)
 {
@@ -67,7 +67,7 @@ template <int NP, class T, bool NT> __global__ __launch_bounds__(kBlock) void ap
     for (int i = 0; i < NP; ++i) st<NT>(to + (i + 1) * slot, mv[i]);
 }
 
-// A page of one slot is contiguous over its heads; a thread moves 16 bytes (48 pages of three parties, 2 x 4 MB each: 70 us, 5.7 TB/s; with four or eight
+// A page of one slot is contiguous over its heads; a thread moves 16 bytes (48 pages of three parties, 2 x 4 MB each: 71 us, 5.7 TB/s; with four or eight
 // a thread 74 and 77, with ordinary accesses 80).  blockIdx.y = pair, blockIdx.z = slot and pool.
 template <class T, bool NT>
 __global__ __launch_bounds__(kBlock) void copy_kernel(CacheView c, const int32_t *src, const int32_t *dst, T *K, T *V)

@@ -127,7 +127,9 @@ template <class T> __device__ inline void put_at_bytes(T *scalar, u32 bytes, T v
 // has one party.
 //
 // HBM bounds it (a tile of 16 rows of three parties takes 64 KB of cache and 432 MFMA, a sixth of the time), if enough is in flight: a wave has the loads of
-// two slots in flight, over the ends of k-tiles and runs, and reads all of a score's triple and tuple words at once.
+// two slots in flight, over the ends of k-tiles and runs, and reads all of a score's triple and tuple words at once.  3 parties, one token, 8 heads of 128:
+// 4 sequences of up to 32768 455 us, 5.0 TB/s.  Shorter calls wait for their beginnings and ends, two workgroups a CU: trees of 8, 16 heads over 4, two sequences of up to
+// 8192 118 us (88 without the products; two row tiles a workgroup 116); two of up to 700, 8 heads of 64, 12 us, a chain of look-ups, loads, digits and one wave's products.
 constexpr int kScoreWanted = 2048;     // workgroups
 constexpr int kScoreWaves = 4, kScoreBlock = 64 * kScoreWaves;
 
@@ -367,6 +369,9 @@ __global__ __launch_bounds__(kScoreBlock, sizeof(T) == 8 ? 2 : NP < 6 ? 4 : 3) v
 // digits written by one thread.  The rows' digits of the next 64 tokens are split into the other half of LDS while the matrix cores work on these; a wave has the loads
 // of two slots in flight, over the turns' ends.  Sums as above; eight pairs and two products of at most 2^14 a token and party, so a range is at
 // most kMostTokens long (16 x 8 x 512 x 2^14 = 2^30).
+//
+// HBM bounds long calls: 3 parties' 16 heads over 4 x 8 x 128, one token, up to 32769 cached, 379 us, 5.75 TB/s.  With more rows it is the digits of P and A, which
+// all column blocks make anew: 2 parties' 32-bit trees of 7, 20 heads over 8 x 4 x 80, up to 3008 cached, 39 us, 5 of them the join of the ranges.
 constexpr int kMostTokens = 512 * SPIN_MAX_PARTIES;        // times parties
 
 // One element of the result whose parties' products sum to z, truncated.

@@ -58,7 +58,7 @@ __device__ inline void add_to(u32 *p, u32 v) { atomicAdd(p, v); }
 // A thread keeps to one diagonal, so its bucket never changes and its sum stays in a register; neighbouring threads read neighbouring words of a row.  The
 // rows of a diagonal that are there are an interval, so the loop over them has no condition and eight loads are in flight.  A workgroup's sums meet in LDS, one global
 // addition a bucket is left; ring additions commute, so their order changes nothing.  Rows start anywhere in a cache line, which neighbouring waves share: with
-// non-temporal loads, which fetch those lines twice, 3 parties' 4 x 16 x 1000 x 1000 take 431 us, with these 354.  159 us for a decoder's 4 x 16 x 1024 x 1024, half of
+// non-temporal loads, which fetch those lines twice, 3 parties' 4 x 16 x 1000 x 1000 take 431 us, with these 354.  158 us for a decoder's 4 x 16 x 1024 x 1024, half of
 // which is read: 5 TB/s.
 // blockIdx.x = block of diagonals, blockIdx.y = run of rows and of sequences, blockIdx.z = party and head.
 constexpr int kMostBuckets = 1024;
