@@ -2,10 +2,9 @@
 //
 // A ring word is rewritten as ND balanced digits of eight bits (limb_common.hpp); a product of words is the sum over digit pairs i + j < ND on
 // v_mfma_i32_16x16x64_i8, pairs of one diagonal sharing an accumulator: 36 int8 products a multiply-add of 64-bit words, 10 of 32-bit ones.
-// The cache stays in ring words, read once from HBM straight into the registers of the wave that multiplies them and split there: a lane's 16 k of a
-// fragment may be any 16 as long as both factors take the same, so they are those that its 16-byte loads bring,
-//     k(j, h, e) = 4 W j + W h + e       (W words in 16 bytes, h = lane / 16, e < W),
-// which makes the four lanes of a row read 64 bytes side by side.  The new tokens' factor (E and every A_i, 16 rows) is split once a workgroup
+// The cache stays in ring words, read once from HBM into the registers of the wave that multiplies them and split there.  A lane's 16 k of a
+// fragment may be any 16 as long as both factors take the same, here two of the 16-byte pieces of each line of 128,
+//     k(j, h, e) = 4 W j + W h + e       (W words in 16 bytes, h = lane / 16, e < W).  The new tokens' factor (E and every A_i, 16 rows) is split once a workgroup
 // into LDS, in fragment order.
 #include "generation.hpp"
 #include "limb_common.hpp"
@@ -127,14 +126,21 @@ template <class T> __device__ inline void put_at_bytes(T *scalar, u32 bytes, T v
 // has one party.
 //
 // HBM bounds it (a tile of 16 rows of three parties takes 64 KB of cache and 432 MFMA, a sixth of the time), if enough is in flight: a wave has the loads of
-// two slots in flight, over the ends of k-tiles and runs, and reads all of a score's triple and tuple words at once.  3 parties, one token, 8 heads of 128:
-// 4 sequences of up to 32768 455 us, 5.0 TB/s.  Shorter calls wait for their beginnings and ends, two workgroups a CU: trees of 8, 16 heads over 4, two sequences of up to
-// 8192 118 us (88 without the products; two row tiles a workgroup 116); two of up to 700, 8 heads of 64, 12 us, a chain of look-ups, loads, digits and one wave's products.
+// two slots in flight, over the ends of k-tiles and runs, and reads all of a score's triple and tuple words at once.  A load instruction takes whole lines, eight lanes a
+// row, and each line is turned in LDS to the four lanes that an MFMA wants of a row: with four lanes a row in the loads themselves 64 bytes are asked for at a time, by
+// 16 lanes in 16 lines, and a token of 4 x 4 heads of 128 over up to 2000 (3 parties) takes 27 us, not 18.  3 parties, four sequences of up to 32768, one token: 8 heads of 128
+// 365 us, 6.0 TB/s; 16 heads over 8 403 us, 5.65.  Calls with work for one round of workgroups wait for its beginning and end: trees of 8, 16 heads over 4, two sequences
+// of up to 8192 111 us (118 with four lanes a row; two row tiles a workgroup the same); one token over two of up to 700, 8 heads of 64, 8.4 us.
 constexpr int kScoreWanted = 2048;     // workgroups
 constexpr int kScoreWaves = 4, kScoreBlock = 64 * kScoreWaves;
+constexpr int kTurn = kTile * 128;     // bytes of a line of 16 rows
+constexpr double kKept = 256 << 20;    // bytes of the Infinity Cache: a cache that is larger and read once is read with non-temporal loads
+// Up to two rows a cached head are multiplied on the vector unit: no digits.  3 parties, a token, 4 cached heads of 128, four sequences of up to 2000, 64-bit words: one
+// row 17.9 us, by matrix units 26.0; two 21.6 and 26.0; four 29.3 and 27.4.  32-bit words: one 11.4 and 14.3; four 15.8 and 15.0.
+constexpr int kFewRows = 2;
 
-template <int NP, class T, bool SUM>
-__global__ __launch_bounds__(kScoreBlock, sizeof(T) == 8 ? 2 : NP < 6 ? 4 : 3) void scores_kernel(AttentionArgs<T> a, int runs, int held)
+template <int NP, class T, bool SUM, bool FEW, bool NT>
+__global__ __launch_bounds__(kScoreBlock, sizeof(T) == 8 ? 2 : NP < (FEW ? 6 : 5) ? 4 : 3) void scores_kernel(AttentionArgs<T> a, int runs, int held)
 {
     using L = Lane<T>;
     constexpr int ND = L::ND, W = L::W, STEPS = SUM ? NP + 1 : 2;
@@ -188,10 +194,37 @@ __global__ __launch_bounds__(kScoreBlock, sizeof(T) == 8 ? 2 : NP < 6 ? 4 : 3) v
             }
         }
     };
+    // The same as words for the vector unit: [slot][row][k].
+    const int row_words = k_tiles * kDepth, few_words = R * row_words;
+    auto stage_words = [&]() __attribute__((always_inline)) {
+        for (int c = threadIdx.x; c < few_words / W; c += kScoreBlock) {
+            const int row = c * W / row_words, at = c * W % row_words;
+            const bool there = at < dim;
+            const size_t from = (first_row + row) * dim + (there ? at : 0);
+            vec q[NP], m[NP], e;
+#pragma unroll
+            for (int i = 0; i < NP; ++i) {
+                q[i] = *(const vec *)(a.x + i * rows * dim + from);
+                m[i] = *(const vec *)(a.A + i * rows * dim + from);
+            }
+#pragma unroll
+            for (int k = 0; k < W; ++k) {
+                e[k] = 0;
+#pragma unroll
+                for (int i = 0; i < NP; ++i) {
+                    e[k] += there ? q[i][k] - m[i][k] : 0;
+                    m[i][k] = there ? m[i][k] : 0;
+                }
+            }
+            ((vec *)lds)[c] = e;
+#pragma unroll
+            for (int i = 0; i < NP; ++i) ((vec *)lds)[(i + 1) * (few_words / W) + c] = m[i];
+        }
+    };
     const size_t slot = ((size_t)a.c.pages * a.c.heads << a.c.shift) * dim;
     const T *slots = a.pool + (SUM ? 0 : party * slot);    // the one that party's slot comes after
-    const u32 lane_row = lane % 16 * dim * sizeof(T), lane_at = lane_row + h * W * sizeof(T);  // 16 tokens are on one page: a scalar address and these bytes
-    vec raw[2][L::loads];
+    const u32 lane_row = lane / 8 * dim * sizeof(T), lane_at = lane_row + lane % 8 * W * sizeof(T);  // 16 tokens are on one page: a scalar address and these bytes
+    vec raw[FEW ? 3 : 2][L::loads];
     // The words of a step; past a row's end the rows' digits are zero, whatever is read.  No load stands behind a branch: its register would be copied where the
     // branches meet, and a copy waits for the load.
     auto load = [&](vec (&v)[L::loads], int s, int kt, size_t key) __attribute__((always_inline)) {
@@ -200,8 +233,9 @@ __global__ __launch_bounds__(kScoreBlock, sizeof(T) == 8 ? 2 : NP < 6 ? 4 : 3) v
         asm volatile("" : "+s"(begin_of));                 // addresses are made here, not carried along for every slot and j
 #pragma unroll
         for (int j = 0; j < L::loads; ++j) {
-            const int at = begin_of + j * (4 * W);         // a row's end is a multiple of 8
-            v[j] = *(const vec *)(from + (at < dim ? at : 0) * sizeof(T) + (4 * W <= 8 || at + h * W < dim ? lane_at : lane_row));
+            const int at = begin_of + j / 2 * (8 * W);     // a row's end is a multiple of 8
+            const vec *const piece = (const vec *)(from + (j % 2 * 8 * dim + (at < dim ? at : 0)) * sizeof(T) + (at + lane % 8 * W < dim ? lane_at : lane_row));
+            v[j] = NT ? __builtin_nontemporal_load(piece) : *piece;
         }
     };
     int page = 0;
@@ -215,7 +249,11 @@ __global__ __launch_bounds__(kScoreBlock, sizeof(T) == 8 ? 2 : NP < 6 ? 4 : 3) v
     const int my_row = min(row0 + (int)threadIdx.x % kTile, R - 1);
     const u64 my_tree = tree_row(a.d, b, my_row % a.d.nodes);
     const int my_place = place(my_row % a.d.nodes), my_bucket = a.bias.table ? bucket_at(a.bias, -a.bias.reach) : -1;
-    const bool whole = held >= k_tiles;
+    const bool whole = FEW || held >= k_tiles;
+    // Where a wave turns a line of 16 rows: piece p of row r in place p ^ (r / 2 % 8), which keeps 16 lanes off each other's banks both ways.
+    char *const turn = lds + (NP + 1) * held * (ND * kFrag) + wave * kTurn;
+    const u32 turn_in = lane / 8 * 128 + ((lane % 8) ^ (lane / 16)) * 16, turn_in8 = lane / 8 * 128 + ((lane % 8) ^ (4 + lane / 16)) * 16;
+    const u32 turn_out = lane % 16 * 128 + (h ^ (lane % 16 / 2)) * 16;
     size_t key = key_of(begin);
     const int active = begin < limit ? min(runs, (limit - begin + kDepth - 1) / kDepth) : 0;   // runs with something to see
     const size_t each = rows * a.d.columns;
@@ -240,7 +278,12 @@ __global__ __launch_bounds__(kScoreBlock, sizeof(T) == 8 ? 2 : NP < 6 ? 4 : 3) v
                 pre[3][i] = at_bytes(a.r_msb + (i * each + corner), at);
             }
         }
-        if (whole) stage(0, k_tiles);
+        if constexpr (FEW) {
+            if constexpr (STEPS > 2) load(raw[2], 2, 0, key);
+            stage_words();
+        } else if (whole) {
+            stage(0, k_tiles);
+        }
     }
     if (threadIdx.x < kTile) {
         row_tree[threadIdx.x] = my_tree;
@@ -256,6 +299,7 @@ __global__ __launch_bounds__(kScoreBlock, sizeof(T) == 8 ? 2 : NP < 6 ? 4 : 3) v
     v4i acc[ND];
 #pragma unroll
     for (int d = 0; d < ND; ++d) acc[d] = v4i{0, 0, 0, 0};
+    T z_few[kFewRows][2] = {};                             // tokens lane / 8 and 8 further
     int kt = 0, here = page;
     size_t next = 0;
     // One loop over k-tiles and runs, so that the loads of the next k-tile's first two steps are under way whichever run it belongs to; behind the last one
@@ -273,13 +317,53 @@ __global__ __launch_bounds__(kScoreBlock, sizeof(T) == 8 ? 2 : NP < 6 ? 4 : 3) v
             stage(kt, 1);
             __syncthreads();
         }
+        if constexpr (FEW) {
+            const vec *left = (const vec *)lds + kt * (kDepth / W) + lane % 8;
+#pragma unroll
+            for (int s = 1; s < STEPS; ++s) {
+                vec (&w)[L::loads] = raw[2 - s % 2];
+                const vec *mask = left + (SUM ? s : party + 1) * (few_words / W);
+#pragma unroll
+                for (int r = 0; r < kFewRows; ++r) {
+                    if (r >= R) break;
+#pragma unroll
+                    for (int j = 0; j < L::loads / 2; ++j) {
+                        const vec e = left[r * (row_words / W) + 8 * j], m = mask[r * (row_words / W) + 8 * j];
+#pragma unroll
+                        for (int g = 0; g < 2; ++g) {
+#pragma unroll
+                            for (int k = 0; k < W; ++k) z_few[r][g] += e[k] * w[2 * j + g][k] + m[k] * raw[0][2 * j + g][k];
+                            computed_here(z_few[r][g]);
+                        }
+                        if (j % 2) __builtin_amdgcn_sched_barrier(0);
+                    }
+                }
+                __builtin_amdgcn_sched_barrier(0);         // these registers are the loads' from here on
+                if (s + 2 < STEPS) load(w, s + 2, kt, key);
+                else load(w, 2 - s % 2, kt1, key1);
+                if (s + 1 == STEPS) load(raw[0], 0, kt1, key1);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        }
         const char *left = lds + (whole ? kt : 0) * (ND * kFrag) + lane * 16;
         v4i f[ND], right[ND];
 #pragma unroll
-        for (int s = 0; s < STEPS; ++s) {
+        for (int s = 0; s < (FEW ? 0 : STEPS); ++s) {
             T w[16];
 #pragma unroll
-            for (int j = 0; j < 16; ++j) w[j] = raw[s % 2][j / W][j % W];
+            for (int j = 0; j < L::loads; j += 2) {        // 16 lines: eight lanes a row in, four lanes a row out; the wave's own LDS, whose accesses stay in order
+                *(vec *)(turn + turn_in) = raw[s % 2][j];
+                *(vec *)(turn + 8 * 128 + turn_in8) = raw[s % 2][j + 1];
+                __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+                __builtin_amdgcn_wave_barrier();
+                __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+                const vec low = *(const vec *)(turn + turn_out), high = *(const vec *)(turn + (turn_out ^ 64));
+                __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+                __builtin_amdgcn_wave_barrier();
+                __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+#pragma unroll
+                for (int k = 0; k < W; ++k) w[j * W + k] = low[k], w[(j + 1) * W + k] = high[k];
+            }
             split<T>(w, s == 0 ? f : right);
             __builtin_amdgcn_sched_barrier(0);             // these registers are the loads' of two steps on
             if (s + 2 < STEPS) load(raw[s % 2], s + 2, kt, key);
@@ -300,7 +384,7 @@ __global__ __launch_bounds__(kScoreBlock, sizeof(T) == 8 ? 2 : NP < 6 ? 4 : 3) v
         int quarter = h;
         asm volatile("" : "+v"(quarter));
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
+        for (int r = 0; r < (FEW ? 1 : 4); ++r) {
             if (NP > 3) __builtin_amdgcn_sched_barrier(0); // a score's words at a time
             if (row0 + 4 * r >= R) break;
             const int row = row0 + 4 * r + quarter;
@@ -317,7 +401,24 @@ __global__ __launch_bounds__(kScoreBlock, sizeof(T) == 8 ? 2 : NP < 6 ? 4 : 3) v
             auto bias_of = [&](int i) __attribute__((always_inline)) {
                 return far ? row_far[i][4 * r + quarter] : bucket < 0 ? 0 : bias[(size_t)i * a.heads * a.bias.buckets + bucket];
             };
-            T z = recombine<T>(acc, r);
+            T z = 0;
+            if constexpr (FEW) {
+#pragma unroll
+                for (int k = 0; k < kFewRows; ++k) {
+                    if (k >= R) break;
+#pragma unroll
+                    for (int g = 0; g < 2; ++g) {
+                        T v = z_few[k][g];                 // the eight lanes of a token have an eighth of k each
+#pragma unroll
+                        for (int by = 1; by < 8; by *= 2) v += __shfl_xor(v, by);
+                        v = __shfl(v, lane % 8 * 8);
+                        z = h == k && lane % 16 / 8 == g ? v : z;
+                        z_few[k][g] = 0;
+                    }
+                }
+            } else {
+                z = recombine<T>(acc, r);
+            }
             if constexpr (SUM) {
                 Opened<T> c{a.f};
                 c.add(z);
@@ -614,7 +715,6 @@ template <int NP, class T> __global__ __launch_bounds__(kFewBlock) void few_valu
 }
 
 inline int value_waves(int dim) { return dim <= 4 * kTile ? 4 : 8; }
-constexpr double kKept = 256 << 20;    // bytes of the Infinity Cache
 // Tiles of 16 rows a workgroup: two where there are more rows than one has, and registers and LDS for it.  2 parties' 16 heads over 4 cached ones, 16 nodes, two
 // sequences of up to 6016: 95 us, 110 by single tiles; 32-bit words, 35 rows of eight sequences: 40 and 44; 20 and 32 rows of 3 parties: 78 and 78, 96 and 96.
 constexpr bool two_value_tiles(int n, int word_bytes) { return n <= (word_bytes == 8 ? 3 : 2); }
@@ -651,26 +751,37 @@ size_t cache_values_workspace(int n, int batch, int heads, int cached_heads, int
 template <class T> spin_status launch_cache_scores(const AttentionArgs<T> &a, hipStream_t s)
 {
     KernelTimer timer(SPIN_KERNEL_ATTENTION, s);
-    constexpr int kMostLds = 158 << 10;                    // and up to 1.2 KB for what belongs to the rows
+    constexpr int kMostLds = 150 << 10;                    // and up to 1.2 KB for what belongs to the rows
     const int R = a.heads / a.c.heads * a.d.nodes, row_tiles = (R + kTile - 1) / kTile, k_tiles = (a.c.dim + kDepth - 1) / kDepth;
+    // 3 parties, a token, four sequences of up to 32768: 8 heads of 128 366 us, 408 with ordinary loads; 32-bit words 191 and 214.  Read twice (two row tiles) 120 and 117.
+    const bool streamed = row_tiles == 1 && (double)(a.n + 1) * a.batch * a.c.heads * a.d.columns * a.c.dim * sizeof(T) > kKept;
     spin_status st = SPIN_OK;
     for_party_count(a.n, [&](auto np) {
         constexpr int NP = decltype(np)::value, kSlots = (NP + 1) * (int)sizeof(T) * kFrag;
         const int held = k_tiles * kSlots <= kMostLds ? k_tiles : 1;
+        const bool few = R <= kFewRows;
         const long blocks = ((long)a.d.columns + kDepth - 1) / kDepth, groups = (long)row_tiles * a.c.heads * a.batch;
         long runs = blocks * groups / kScoreWanted;
         runs = runs < 1 ? 1 : runs > 16 ? 16 : runs;
         const long strips = ((blocks + runs - 1) / runs + kXcds - 1) / kXcds;
-        auto go = [&](auto sum) {
-            constexpr bool SUM = decltype(sum)::value;
+        auto go = [&](auto sum, auto by_words, auto nt) {
+            constexpr bool SUM = decltype(sum)::value, FEW = decltype(by_words)::value, NT = decltype(nt)::value;
             static OncePerDevice lds_flags;
-            st = allow_dynamic_lds((const void *)scores_kernel<NP, T, SUM>, kMostLds, lds_flags);
+            st = allow_dynamic_lds((const void *)scores_kernel<NP, T, SUM, FEW, NT>, kMostLds + kScoreWaves * kTurn, lds_flags);
             if (st != SPIN_OK) return;
             const dim3 grid((unsigned)(strips * kXcds * row_tiles), a.c.heads, SUM ? a.batch : a.batch * NP);
-            scores_kernel<NP, T, SUM><<<grid, kScoreBlock, held * kSlots, s>>>(a, (int)runs, held);
+            const int bytes = FEW ? (NP + 1) * R * k_tiles * kDepth * (int)sizeof(T) : held * kSlots + kScoreWaves * kTurn;
+            scores_kernel<NP, T, SUM, FEW, NT><<<grid, kScoreBlock, bytes, s>>>(a, (int)runs, held);
         };
-        if (a.f) go(std::true_type());
-        else go(std::false_type());
+        auto with = [&](auto sum) {
+            if constexpr (decltype(sum)::value) {
+                if (streamed) return few ? go(sum, std::true_type(), std::true_type()) : go(sum, std::false_type(), std::true_type());
+            }
+            if (few) go(sum, std::true_type(), std::false_type());
+            else go(sum, std::false_type(), std::false_type());
+        };
+        if (a.f) with(std::true_type());
+        else with(std::false_type());
     });
     return st != SPIN_OK ? st : check_launch("spin_cache_scores");
 }
@@ -681,8 +792,7 @@ template <class T> spin_status launch_cache_values(const AttentionArgs<T> &a, hi
     const int R = a.heads / a.c.heads * a.d.nodes, range = value_range(a.n, a.batch, a.heads, a.c.heads, a.d.nodes, a.d.columns, a.c.dim, sizeof(T));
     const int ranges = (a.d.columns - 1) / range + 1, strips = (ranges + kXcds - 1) / kXcds;
     T *partial = ranges > 1 ? (T *)a.workspace : nullptr;
-    // A cache larger than what the chip keeps, read once: non-temporal loads, where a wave's 16 words are whole cache lines (64-bit words, rows of whole tiles) and no
-    // other row tile reads them.  3 parties' 4 x 8 heads over up to 32769 tokens 382 us, 405 with ordinary loads; 32-bit words, half a line, 231 and 208.
+    // Non-temporal where a wave's 16 words are whole cache lines (64-bit words, rows of whole tiles) and no other row tile reads them.  3 parties' 4 x 8 heads over up to 32769 tokens 382 us, 405 with ordinary loads; 32-bit words, half a line, 231 and 208.
     const bool streamed = R <= kTile && a.c.dim % kTile == 0 &&
                           (double)(a.n + 1) * a.batch * a.c.heads * a.d.columns * a.c.dim * sizeof(T) > kKept;
     spin_status st = SPIN_OK;

@@ -372,3 +372,21 @@ def test_values_of_a_wide_call_with_short_contexts(n, heads, dim, context):
     want = gen.values(pool, table, np.array([context]), P[..., :short], A[..., :short], C, 16, tup, tree)
     got = spin.cache_values(dev(pool), ints(table), ints([context]), dev(P), dev(A), dev(C), f=16, tuple_=[dev(t) for t in tup], tree=dev(tree))
     assert same(got, want)
+
+
+@BITS
+@pytest.mark.parametrize("n,heads,nodes,dim", [(2, 1, 1, 128), (3, 1, 2, 72), (2, 4, 3, 128), (5, 3, 5, 40)])
+def test_scores_of_a_wide_call_with_short_contexts(bits, n, heads, nodes, dim):
+    """The same for keys, by words (up to two rows) and by digits."""
+    ring, unsigned, _ = RINGS[bits]
+    rng = np.random.default_rng(dim + nodes)
+    columns, context = (1 << 31) // (bits * (n + 1) * dim) + 77, 150
+    pool, table = uniform(rng, bits, n + 1, 14, 1, 16, dim), table_of(rng, 1, 12, 14)
+    Q, A = uniform(rng, bits, n, 1, heads, nodes, dim), uniform(rng, bits, n, 1, heads, nodes, dim)
+    C = uniform(rng, bits, n, 1, heads, nodes, columns)
+    tup = tuple_of(rng, bits, C.shape)
+    short = 12 * 16 + 3
+    want = gen.scores(pool, table, np.array([context]), Q, A, C[..., :short], 9, tuple(t[..., :short] for t in tup), masked=5)
+    got = ring.cache_scores(dev(pool), ints(table), ints([context]), dev(Q), dev(A), dev(C), f=9, tuple_=[dev(t) for t in tup], masked=5)
+    assert same(got[..., :short].contiguous(), want)
+    assert (got[0, ..., short:] == 5).all() and not got[1:, ..., short:].any()
