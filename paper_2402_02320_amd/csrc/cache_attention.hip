@@ -471,7 +471,7 @@ __global__ __launch_bounds__(kScoreBlock, sizeof(T) == 8 ? 2 : NP < (FEW ? 6 : 5
 // of two slots in flight, over the turns' ends.  Sums as above; eight pairs and two products of at most 2^14 a token and party, so a range is at
 // most kMostTokens long (16 x 8 x 512 x 2^14 = 2^30).
 //
-// HBM bounds long calls: 3 parties' 16 heads over 4 x 8 x 128, one token, up to 32769 cached, 379 us, 5.75 TB/s.  With more rows it is the digits of P and A, which
+// HBM bounds long calls (few rows: below).  With more rows it is the digits of P and A, which
 // all column blocks make anew: 2 parties' 32-bit trees of 7, 20 heads over 8 x 4 x 80, up to 3008 cached, 39 us, 5 of them the join of the ranges.
 constexpr int kMostTokens = 512 * SPIN_MAX_PARTIES;        // times parties
 
@@ -655,6 +655,135 @@ __global__ __launch_bounds__(64 * WAVES, sizeof(T) == 8 || NP > 6 ? 2 : 4) void 
     }
 }
 
+// Up to few_value_rows() rows a cached head: on the vector unit, a lane 16 bytes of a cached row, so that a load takes whole rows: `tokens` of them where they are short (up to 16,
+// of one page).  A wave has every fourth group of tokens of 64; the rows' words of the next 64 are put into LDS, E and the A_i of a token side by side, behind the products
+// of these.  HBM bounds it: 3 parties, a token, four sequences of up to 32769, 16 heads over 8 of 128 355 us, 6.1 TB/s, by matrix units 378; two parties' 8 heads, eight of up
+// to 4097 81 and 111; of up to 2000, 3 parties' 4 heads 20.5 and 29.9, four rows a head 27.6 and 31.1, 32-bit words 17.4 and 15.0; 2 x 4 heads of 64 over 101 9.7 and 12.3.
+// Two sets of buffers: the loads of the next kAtOnce groups are under way during the products of the last.
+constexpr int few_value_rows(int word_bytes) { return word_bytes == 8 ? 4 : 2; }
+template <int NP, class T, bool SUM, bool NT>
+__global__ __launch_bounds__(kScoreBlock, 3) void row_values_kernel(AttentionArgs<T> a, int range, T *partial)
+{
+    constexpr int kMost = few_value_rows(sizeof(T));
+    constexpr int W = 16 / sizeof(T), SLOTS = SUM ? NP + 1 : 2, kAtOnce = SLOTS <= 4 ? 2 : 1, kWords = 2 * kDepth * kMost * (NP + 1), kSums = kScoreBlock * kMost * W;
+    typedef T vec __attribute__((ext_vector_type(W)));
+    __shared__ __align__(16) T lds[kWords > kSums ? kWords : kSums];
+    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    const int b = SUM ? blockIdx.z : blockIdx.z / NP, party = SUM ? 0 : blockIdx.z % NP, dim = a.c.dim;
+    const int share = a.heads / a.c.heads, R = share * a.d.nodes, all = dim / W, column_blocks = (all + 63) / 64, lanes = min(all, 64);
+    int block, row0;
+    place_of(1, kMost, block, row0);
+    const int g = blockIdx.y / column_blocks, col = (blockIdx.y % column_blocks * 64 + lane % lanes) * W;
+    const size_t rows = (size_t)a.batch * a.heads * a.d.nodes, first_row = ((size_t)b * a.heads + (size_t)g * share) * a.d.nodes;
+    const int context = a.d.context[b];
+    const int limit = context < 0 ? 0 : (int)min((long)a.d.columns, (long)context + a.d.nodes);
+    if ((long)block * range >= a.d.columns) return;
+    const int begin = block * range, end = min(begin + range, limit);
+    const int tokens = min(1 << (31 - __clz(64 / lanes)), kTile), steps = kTile / tokens, batches = (steps + kAtOnce - 1) / kAtOnce;       // a wave and 64 tokens
+    const int sub = lane / lanes;
+    const bool mine = sub < tokens && col < dim;
+    const u32 lane_at = mine ? (sub * dim + col) * (u32)sizeof(T) : 0;
+
+    auto stage = [&](int t0, T *to) __attribute__((always_inline)) {
+        const int row = threadIdx.x / kDepth, t = t0 + threadIdx.x % kDepth;
+        if (row >= R) return;
+        const bool seen = t < end && page_of(a.c, b, t) >= 0 && sees(tree_row(a.d, b, row % a.d.nodes), a.d.nodes, context, t);
+        const size_t from = (first_row + row) * a.d.columns + min(t, a.d.columns - 1);
+        T x[NP], m[NP], e = 0;
+#pragma unroll
+        for (int i = 0; i < NP; ++i) x[i] = a.x[i * rows * a.d.columns + from], m[i] = a.A[i * rows * a.d.columns + from];
+        to += (threadIdx.x % kDepth * R + row) * (NP + 1);
+#pragma unroll
+        for (int i = 0; i < NP; ++i) {
+            e += seen ? x[i] - m[i] : 0;
+            to[i + 1] = seen ? m[i] : 0;
+        }
+        to[0] = e;
+    };
+    const size_t slot = ((size_t)a.c.pages * a.c.heads << a.c.shift) * dim;
+    const T *slots = a.pool + (SUM ? 0 : party * slot);
+    const auto *table = (const __attribute__((address_space(4))) int32_t *)(uintptr_t)(a.c.table + (size_t)b * a.c.table_pages);
+    // The groups of a batch; behind the last one, and where a page is not there, some rows of the pool, which are multiplied by zero or not at all.
+    auto load = [&](vec (&v)[kAtOnce][SLOTS], int t0, int batch) __attribute__((always_inline)) {
+#pragma unroll
+        for (int j = 0; j < kAtOnce; ++j) {
+            const int t = t0 + (min(batch * kAtOnce + j, steps - 1) * kScoreWaves + wave) * tokens, page = table[min(t >> a.c.shift, a.c.table_pages - 1)];
+            const size_t base = row_at(a.c, 0, (unsigned)page < (unsigned)a.c.pages ? page : 0, g, t);
+#pragma unroll
+            for (int s = 0; s < SLOTS; ++s) {
+                const vec *p = (const vec *)((const char *)((s == 0 ? a.pool : slots + s * slot) + base) + lane_at);
+                v[j][s] = NT ? __builtin_nontemporal_load(p) : *p;
+            }
+        }
+    };
+    T z[kMost][W] = {};
+    auto multiply_words = [&](const vec (&v)[kAtOnce][SLOTS], const T *from, int batch) __attribute__((always_inline)) {
+#pragma unroll
+        for (int j = 0; j < kAtOnce; ++j) {
+            if (batch * kAtOnce + j >= steps) break;
+            const T *factors = from + (((batch * kAtOnce + j) * kScoreWaves + wave) * tokens + min(sub, tokens - 1)) * R * (NP + 1);
+#pragma unroll
+            for (int r = 0; r < kMost; ++r) {
+                if (r >= R) break;
+                const T e = factors[r * (NP + 1)];
+#pragma unroll
+                for (int s = 1; s < SLOTS; ++s) {
+                    const T m = factors[r * (NP + 1) + (SUM ? s : party + 1)];
+#pragma unroll
+                    for (int k = 0; k < W; ++k) z[r][k] += e * v[j][s][k] + m * v[j][0][k];
+                }
+#pragma unroll
+                for (int k = 0; k < W; ++k) computed_here(z[r][k]);
+            }
+        }
+    };
+    vec raw[2][kAtOnce][SLOTS];
+    if (begin < end) {
+        load(raw[0], begin, 0);
+        stage(begin, lds);
+    }
+    int t0 = begin, batch = 0, half = 0;
+    __syncthreads();
+    // Two batches a turn of the loop, so that each set of buffers has its place in registers.
+    while (t0 < end) {
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            if (t0 >= end) break;
+            const bool last = batch + 1 == batches;
+            __builtin_amdgcn_sched_barrier(0);
+            load(raw[1 - k], last ? min(t0 + kDepth, end - 1 & ~(kDepth - 1)) : t0, last ? 0 : batch + 1);
+            __builtin_amdgcn_sched_barrier(0);
+            multiply_words(raw[k], lds + half * (kWords / 2), batch);
+            ++batch;
+            if (last) {
+                t0 += kDepth;
+                batch = 0;
+                half ^= 1;
+                if (t0 < end) stage(t0, lds + half * (kWords / 2));
+                __syncthreads();
+            }
+        }
+    }
+    // The waves' and groups' sums.
+    const size_t each = rows * dim;
+#pragma unroll
+    for (int r = 0; r < kMost; ++r)
+#pragma unroll
+        for (int k = 0; k < W; ++k) lds[(r * W + k) * kScoreBlock + threadIdx.x] = mine ? z[r][k] : 0;
+    __syncthreads();
+    for (int c = threadIdx.x; c < R * W * lanes; c += kScoreBlock) {
+        const int part = c / lanes, l = c % lanes, column = (blockIdx.y % column_blocks * 64 + l) * W + part % W;
+        if (column >= dim) continue;
+        T sum = 0;
+        for (int w = 0; w < kScoreWaves; ++w)
+            for (int k = 0; k < tokens; ++k) sum += lds[part * kScoreBlock + w * 64 + k * lanes + l];
+        const size_t at = (first_row + part / W) * dim + column;
+        if (partial) partial[((size_t)block * (SUM ? 1 : NP) + party) * each + at] = sum;
+        else if constexpr (SUM) finish<NP, T>(a, at, each, sum);
+        else a.out[party * each + at] = a.C[party * each + at] + sum;
+    }
+}
+
 // Adds the ranges' parts: kJoinRows threads an element (of one party where SUM is false), each every kJoinRows-th range.
 constexpr int kJoinRows = 4, kJoinBlock = 256;
 template <int NP, class T, bool SUM> __global__ __launch_bounds__(kJoinBlock) void join_kernel(AttentionArgs<T> a, int ranges, const T *partial)
@@ -714,6 +843,7 @@ template <int NP, class T> __global__ __launch_bounds__(kFewBlock) void few_valu
     }
 }
 
+constexpr double kFewSlots = 3;        // workgroups a CU of row_values_kernel
 inline int value_waves(int dim) { return dim <= 4 * kTile ? 4 : 8; }
 // Tiles of 16 rows a workgroup: two where there are more rows than one has, and registers and LDS for it.  2 parties' 16 heads over 4 cached ones, 16 nodes, two
 // sequences of up to 6016: 95 us, 110 by single tiles; 32-bit words, 35 rows of eight sequences: 40 and 44; 20 and 32 rows of 3 parties: 78 and 78, 96 and 96.
@@ -721,19 +851,21 @@ constexpr bool two_value_tiles(int n, int word_bytes) { return n <= (word_bytes 
 inline int value_tiles(int n, int rows, int dim, int word_bytes) { return rows > kTile && value_waves(dim) == 8 && two_value_tiles(n, word_bytes) ? 2 : 1; }
 
 // Tokens a workgroup, by an estimate: the chip holds `slots` workgroups, of each of which a beginning takes 0.7 of a turn, and with sequences of any length the
-// last round of them is half empty on either side.  us by ranges of 1, 2, 4, 8 turns, the chosen one in brackets: 3 parties' 2 x 8 heads of 64 over 701 tokens
+// last round of them is half empty on either side.  us by matrix units and ranges of 1, 2, 4, 8 turns, the chosen one in brackets: 3 parties' 2 x 8 heads of 64 over 701 tokens
 // [13.9] 18.6 28.9 50.2; 4 x 8 heads of 128 over up to 32769 569 471 422 [402] (16: 487); 2 parties' 8 x 8 over up to 4097 138 112 [111] 176, 32-bit
-// words, 8 x 4 heads of 80 and 35 rows over up to 3008 54 [44] 47 46.
+// words, 8 x 4 heads of 80 and 35 rows over up to 3008 54 [44] 47 46.  By words the same with 2 to 4 workgroups a CU.
 int value_range(int n, int batch, int heads, int cached_heads, int nodes, int columns, int dim, int word_bytes)
 {
+    const bool few = heads / cached_heads * nodes <= few_value_rows(word_bytes);
     const int waves = value_waves(dim), width = waves * kTile, rows = kTile * value_tiles(n, heads / cached_heads * nodes, dim, word_bytes);
     const double groups = (double)batch * cached_heads * ((heads / cached_heads * nodes + rows - 1) / rows) * ((dim + width - 1) / width);
-    const double slots = 256.0 * (8 / waves) * (8 / word_bytes);
+    const double few_groups = (double)batch * cached_heads * ((dim * word_bytes / 16 + 63) / 64);
+    const double slots = few ? 256.0 * kFewSlots : 256.0 * (8 / waves) * (8 / word_bytes);
     const int turns = (columns + kDepth - 1) / kDepth, most = kMostTokens / n / kDepth;
     int best = 1;
     double least = 0;
     for (int r = 1; r <= most && (r == 1 || r < 2 * turns); r *= 2) {
-        const double time = (groups * ((turns + r - 1) / r) / slots + 1) * (0.7 + r);
+        const double time = ((few ? few_groups : groups) * ((turns + r - 1) / r) / slots + 1) * (0.7 + r);
         if (r == 1 || time < least) best = r, least = time;
     }
     return best * kDepth;
@@ -792,9 +924,10 @@ template <class T> spin_status launch_cache_values(const AttentionArgs<T> &a, hi
     const int R = a.heads / a.c.heads * a.d.nodes, range = value_range(a.n, a.batch, a.heads, a.c.heads, a.d.nodes, a.d.columns, a.c.dim, sizeof(T));
     const int ranges = (a.d.columns - 1) / range + 1, strips = (ranges + kXcds - 1) / kXcds;
     T *partial = ranges > 1 ? (T *)a.workspace : nullptr;
-    // Non-temporal where a wave's 16 words are whole cache lines (64-bit words, rows of whole tiles) and no other row tile reads them.  3 parties' 4 x 8 heads over up to 32769 tokens 382 us, 405 with ordinary loads; 32-bit words, half a line, 231 and 208.
-    const bool streamed = R <= kTile && a.c.dim % kTile == 0 &&
-                          (double)(a.n + 1) * a.batch * a.c.heads * a.d.columns * a.c.dim * sizeof(T) > kKept;
+    // By digits, non-temporal where a wave's 16 words are whole cache lines (64-bit words, rows of whole tiles; 32-bit ones, half a line, lose a tenth) and no other row
+    // tile reads them.  3 parties' 4 x 8 heads, four rows over up to 16384 226 us, 235 with ordinary loads; 16 rows over up to 9008 162 and 168.
+    const bool large = (double)(a.n + 1) * a.batch * a.c.heads * a.d.columns * a.c.dim * sizeof(T) > kKept;
+    const bool streamed = R <= kTile && a.c.dim % kTile == 0 && large;
     spin_status st = SPIN_OK;
     for_party_count(a.n, [&](auto np) {
         constexpr int NP = decltype(np)::value;
@@ -803,6 +936,14 @@ template <class T> spin_status launch_cache_values(const AttentionArgs<T> &a, hi
             few_values_kernel<NP, T><<<grid, kFewBlock, 0, s>>>(a);
             return;
         }
+        auto by_words = [&](auto sum, auto nt) {
+            constexpr bool SUM = decltype(sum)::value, NT = decltype(nt)::value;
+            const dim3 grid(strips * kXcds, (a.c.dim * (int)sizeof(T) / 16 + 63) / 64 * a.c.heads, SUM ? a.batch : a.batch * NP);
+            row_values_kernel<NP, T, SUM, NT><<<grid, kScoreBlock, 0, s>>>(a, range, partial);
+            if (!partial) return;
+            const size_t count = (size_t)a.batch * a.heads * a.d.nodes * a.c.dim * (SUM ? 1 : NP), each = kJoinBlock / kJoinRows;
+            join_kernel<NP, T, SUM><<<(unsigned)((count + each - 1) / each), kJoinBlock, 0, s>>>(a, ranges, partial);
+        };
         auto go = [&](auto sum, auto waves, auto tiles, auto nt) {
             constexpr bool SUM = decltype(sum)::value, NT = decltype(nt)::value;
             constexpr int WAVES = decltype(waves)::value, TILES = decltype(tiles)::value, kRows = kTile * TILES, kLds = 2 * TILES * (NP + 1) * (int)sizeof(T) * kFrag;
@@ -826,6 +967,12 @@ template <class T> spin_status launch_cache_values(const AttentionArgs<T> &a, hi
             }
             go(sum, std::integral_constant<int, 8>(), one, std::false_type());
         };
+        if (R <= few_value_rows(sizeof(T))) {
+            if (a.f && large) by_words(std::true_type(), std::true_type());
+            else if (a.f) by_words(std::true_type(), std::false_type());
+            else by_words(std::false_type(), std::false_type());
+            return;
+        }
         if (a.f) with(std::true_type());
         else with(std::false_type());
     });

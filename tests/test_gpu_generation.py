@@ -390,3 +390,46 @@ def test_scores_of_a_wide_call_with_short_contexts(bits, n, heads, nodes, dim):
     got = ring.cache_scores(dev(pool), ints(table), ints([context]), dev(Q), dev(A), dev(C), f=9, tuple_=[dev(t) for t in tup], masked=5)
     assert same(got[..., :short].contiguous(), want)
     assert (got[0, ..., short:] == 5).all() and not got[1:, ..., short:].any()
+
+
+@BITS
+@pytest.mark.parametrize("n,heads,nodes,dim", [(2, 2, 2, 128), (2, 1, 5, 128), (3, 4, 4, 112), (2, 3, 7, 256)])
+def test_values_of_a_wide_call_by_rows(bits, n, heads, nodes, dim):
+    """Values for a cache larger than the chip keeps, of four, five, 16 and 21 rows a cached head."""
+    ring, unsigned, _ = RINGS[bits]
+    rng = np.random.default_rng(dim + nodes)
+    columns, context = (1 << 31) // (bits * (n + 1) * dim) + 77, 171
+    pool, table = uniform(rng, bits, n + 1, 14, 1, 16, dim), table_of(rng, 1, 12, 14)
+    P, A = uniform(rng, bits, n, 1, heads, nodes, columns), uniform(rng, bits, n, 1, heads, nodes, columns)
+    C = uniform(rng, bits, n, 1, heads, nodes, dim)
+    tup, short = tuple_of(rng, bits, C.shape), 12 * 16 + 3
+    want = gen.values(pool, table, np.array([context]), P[..., :short], A[..., :short], C, 9, tup)
+    got = ring.cache_values(dev(pool), ints(table), ints([context]), dev(P), dev(A), dev(C), f=9, tuple_=[dev(t) for t in tup])
+    assert same(got, want)
+
+
+@BITS
+@pytest.mark.parametrize("f", [0, 9])
+@pytest.mark.parametrize("n,share,nodes", [(1, 1, 1), (3, 2, 1), (8, 1, 2), (2, 1, 4), (5, 3, 1), (4, 4, 1)])
+@pytest.mark.parametrize("dim", [8, 24, 40, 72, 104, 136, 200, 256])
+def test_few_rows(bits, f, n, share, nodes, dim):
+    """One to four rows a cached head, heads of every kind of length, a page that is not there, sequences of none to some hundred tokens."""
+    ring, unsigned, _ = RINGS[bits]
+    rng = np.random.default_rng(dim * 31 + n)
+    heads, contexts = 2 * share, [0, 3, 150, 333, -1]
+    pool, table = uniform(rng, bits, n + 1, 120, 2, 16, dim), table_of(rng, len(contexts), 22, 120)
+    table[2, 4], table[3, 0] = -1, 120
+    columns = max(contexts) + nodes + 2
+    Q, A = (uniform(rng, bits, n, len(contexts), heads, nodes, dim) for _ in range(2))
+    C = uniform(rng, bits, n, len(contexts), heads, nodes, columns)
+    tup = tuple_of(rng, bits, C.shape) if f else None
+    tree = rng.integers(0, 1 << nodes, (len(contexts), nodes))
+    ctx = np.array(contexts)
+    put = (lambda t: None if t is None else [dev(x) for x in t])
+    want = gen.scores(pool, table, ctx, Q, A, C, f, tup, tree, masked=7)
+    assert same(ring.cache_scores(dev(pool), ints(table), ints(contexts), dev(Q), dev(A), dev(C), f=f, tuple_=put(tup), tree=dev(tree), masked=7), want)
+    P, A = (uniform(rng, bits, n, len(contexts), heads, nodes, columns) for _ in range(2))
+    C = uniform(rng, bits, n, len(contexts), heads, nodes, dim)
+    tup = tuple_of(rng, bits, C.shape) if f else None
+    want = gen.values(pool, table, ctx, P, A, C, f, tup, tree)
+    assert same(ring.cache_values(dev(pool), ints(table), ints(contexts), dev(P), dev(A), dev(C), f=f, tuple_=put(tup), tree=dev(tree)), want)
