@@ -108,7 +108,7 @@ __device__ inline void place_of(int row_groups, int rows, int &block, int &row0)
     row0 = within / kXcds * rows;
 }
 
-// A word at a scalar address and a lane's bytes from there (rows have at most kMostColumns words, so 16 of them are within 2^31 bytes): no register a lane but
+// A word at a scalar address and a lane's bytes from there (rows have at most kMostColumns words, so 32 of them are within 2^32 bytes): no register a lane but
 // those 32 bits goes into addresses.
 template <bool NT = false, class T> __device__ inline T at_bytes(const T *scalar, u32 bytes)
 {
