@@ -121,5 +121,16 @@ __host__ __device__ inline int bucket_at(const BiasView &v, int distance)
     return (unsigned)b < (unsigned)v.buckets ? b : -1;
 }
 
+// The rows of [q0, q1) whose score on the diagonal k - q = away is there are [from, to): none where to <= from.  Lengths may be anything;
+// |away| and |first| are below 2^30.
+struct DiagonalRows { int from, to; };
+__host__ __device__ inline DiagonalRows rows_of_diagonal(int away, int q0, int q1, int K, int length, bool causal, int first)
+{
+    length = length < 0 ? 0 : length > K ? K : length;     // left negative, the subtraction below can pass 32 bits
+    const int from = q0 > -away ? q0 : -away;
+    if (causal && away > first) return {from, from};
+    return {from, q1 < length - away ? q1 : length - away};
+}
+
 }  // namespace
 }  // namespace spin

@@ -74,9 +74,9 @@ template <class T> __global__ __launch_bounds__(kBlock) void grad_kernel(PairArg
     const int b0 = blockIdx.y / row_runs * sequences, b1 = min(b0 + sequences, a.batch);
     T sum = 0;
     for (int b = b0; b < b1; ++b) {
-        const int length = a.lengths ? min(a.lengths[b], a.K) : a.K;
-        int q = max(q0, -away);
-        const int end = a.causal && away > a.first ? q : min(q1, length - away);
+        const DiagonalRows there = rows_of_diagonal(away, q0, q1, a.K, a.lengths ? a.lengths[b] : a.K, a.causal, a.first);
+        int q = there.from;
+        const int end = there.to;
         const T *x = a.x + ((((size_t)i * a.batch + b) * a.heads + h) * a.Q + q) * a.K + (q + away);
         const size_t step = (size_t)a.K + 1;
         for (; q + 8 <= end; q += 8, x += 8 * step) {
