@@ -880,8 +880,12 @@ size_t cache_values_workspace(int n, int batch, int heads, int cached_heads, int
     return 256 + (ranges > 1 ? ranges * n * batch * heads * nodes * dim * word_bytes : 0);
 }
 
+// The third axis of a launch: sequences, and without truncation, where a workgroup has one party, those times parties.
+template <class T> inline long third_axis(const AttentionArgs<T> &a) { return (long)a.batch * (a.f ? 1 : a.n); }
+
 template <class T> spin_status launch_cache_scores(const AttentionArgs<T> &a, hipStream_t s)
 {
+    if (third_axis(a) > kMaxGrid) return SPIN_ERANGE;
     KernelTimer timer(SPIN_KERNEL_ATTENTION, s);
     constexpr int kMostLds = 150 << 10;                    // and up to 1.2 KB for what belongs to the rows
     const int R = a.heads / a.c.heads * a.d.nodes, row_tiles = (R + kTile - 1) / kTile, k_tiles = (a.c.dim + kDepth - 1) / kDepth;
@@ -920,8 +924,11 @@ template <class T> spin_status launch_cache_scores(const AttentionArgs<T> &a, hi
 
 template <class T> spin_status launch_cache_values(const AttentionArgs<T> &a, hipStream_t s)
 {
+    const int R = a.heads / a.c.heads * a.d.nodes, width = R <= few_value_rows(sizeof(T)) ? 64 * 16 / (int)sizeof(T) : value_waves(a.c.dim) * kTile;
+    const long second_axis = (long)((a.c.dim + width - 1) / width) * a.c.heads;
+    if (a.d.columns > kFewTokens && (third_axis(a) > kMaxGrid || second_axis > kMaxGrid)) return SPIN_ERANGE;
     KernelTimer timer(SPIN_KERNEL_ATTENTION, s);
-    const int R = a.heads / a.c.heads * a.d.nodes, range = value_range(a.n, a.batch, a.heads, a.c.heads, a.d.nodes, a.d.columns, a.c.dim, sizeof(T));
+    const int range = value_range(a.n, a.batch, a.heads, a.c.heads, a.d.nodes, a.d.columns, a.c.dim, sizeof(T));
     const int ranges = (a.d.columns - 1) / range + 1, strips = (ranges + kXcds - 1) / kXcds;
     T *partial = ranges > 1 ? (T *)a.workspace : nullptr;
     // By digits, non-temporal where a wave's 16 words are whole cache lines (64-bit words, rows of whole tiles; 32-bit ones, half a line, lose a tenth) and no other row
@@ -938,7 +945,7 @@ template <class T> spin_status launch_cache_values(const AttentionArgs<T> &a, hi
         }
         auto by_words = [&](auto sum, auto nt) {
             constexpr bool SUM = decltype(sum)::value, NT = decltype(nt)::value;
-            const dim3 grid(strips * kXcds, (a.c.dim * (int)sizeof(T) / 16 + 63) / 64 * a.c.heads, SUM ? a.batch : a.batch * NP);
+            const dim3 grid(strips * kXcds, (unsigned)second_axis, SUM ? a.batch : a.batch * NP);
             row_values_kernel<NP, T, SUM, NT><<<grid, kScoreBlock, 0, s>>>(a, range, partial);
             if (!partial) return;
             const size_t count = (size_t)a.batch * a.heads * a.d.nodes * a.c.dim * (SUM ? 1 : NP), each = kJoinBlock / kJoinRows;
@@ -950,7 +957,7 @@ template <class T> spin_status launch_cache_values(const AttentionArgs<T> &a, hi
             static OncePerDevice lds_flags;
             st = allow_dynamic_lds((const void *)values_kernel<NP, T, SUM, WAVES, TILES, NT>, kLds, lds_flags);
             if (st != SPIN_OK) return;
-            const dim3 grid(strips * kXcds * ((R + kRows - 1) / kRows), (a.c.dim + WAVES * kTile - 1) / (WAVES * kTile) * a.c.heads, SUM ? a.batch : a.batch * NP);
+            const dim3 grid(strips * kXcds * ((R + kRows - 1) / kRows), (unsigned)second_axis, SUM ? a.batch : a.batch * NP);
             values_kernel<NP, T, SUM, WAVES, TILES, NT><<<grid, 64 * WAVES, kLds, s>>>(a, range, partial);
             if (!partial) return;
             const size_t count = (size_t)a.batch * a.heads * a.d.nodes * a.c.dim * (SUM ? 1 : NP), each = kJoinBlock / kJoinRows;

@@ -62,6 +62,7 @@ template <class T> spin_status launch_relbias_grad(const PairArgs<T> &a, hipStre
 
 namespace {
 
+constexpr int kMaxGrid = 65535;        // of a launch grid's second and third axes
 constexpr int kXcds = 8;               // workgroups go to the XCDs in turn
 
 // blockIdx.x, turned on from row to row of the grid so that every XCD meets all of its values: left alone a width that divides into the XCDs gives each of them

@@ -10,7 +10,6 @@ inline bool bad_ptr(const void *p) { return p == nullptr || ((uintptr_t)p & 15) 
 inline bool bad_list(const int32_t *p) { return p == nullptr || ((uintptr_t)p & 3) != 0; }
 inline bool bad_n(int n) { return n < 1 || n > SPIN_MAX_PARTIES; }
 constexpr double kMaxWords = (double)((size_t)1 << 40);  // of any one tensor; offsets are 64 bits
-constexpr int kMaxGrid = 65535;                          // of the launch grids' second and third axes
 
 int log2_of(int v)
 {
