@@ -791,7 +791,7 @@ template <int NP, class T, bool SUM> __global__ __launch_bounds__(kJoinBlock) vo
     constexpr int kElements = kJoinBlock / kJoinRows;
     __shared__ T sums[kJoinBlock];
     const size_t each = (size_t)a.batch * a.heads * a.d.nodes * a.c.dim, count = SUM ? each : NP * each;
-    const size_t at = (size_t)blockIdx.x * kElements + threadIdx.x % kElements;
+    const size_t at = (blockIdx.x + (size_t)blockIdx.y * gridDim.x) * kElements + threadIdx.x % kElements;
     T z = 0;
     if (at < count) {
 #pragma unroll 8
@@ -949,7 +949,7 @@ template <class T> spin_status launch_cache_values(const AttentionArgs<T> &a, hi
             row_values_kernel<NP, T, SUM, NT><<<grid, kScoreBlock, 0, s>>>(a, range, partial);
             if (!partial) return;
             const size_t count = (size_t)a.batch * a.heads * a.d.nodes * a.c.dim * (SUM ? 1 : NP), each = kJoinBlock / kJoinRows;
-            join_kernel<NP, T, SUM><<<(unsigned)((count + each - 1) / each), kJoinBlock, 0, s>>>(a, ranges, partial);
+            join_kernel<NP, T, SUM><<<grid_of((count + each - 1) / each), kJoinBlock, 0, s>>>(a, ranges, partial);
         };
         auto go = [&](auto sum, auto waves, auto tiles, auto nt) {
             constexpr bool SUM = decltype(sum)::value, NT = decltype(nt)::value;
@@ -961,7 +961,7 @@ template <class T> spin_status launch_cache_values(const AttentionArgs<T> &a, hi
             values_kernel<NP, T, SUM, WAVES, TILES, NT><<<grid, 64 * WAVES, kLds, s>>>(a, range, partial);
             if (!partial) return;
             const size_t count = (size_t)a.batch * a.heads * a.d.nodes * a.c.dim * (SUM ? 1 : NP), each = kJoinBlock / kJoinRows;
-            join_kernel<NP, T, SUM><<<(unsigned)((count + each - 1) / each), kJoinBlock, 0, s>>>(a, ranges, partial);
+            join_kernel<NP, T, SUM><<<grid_of((count + each - 1) / each), kJoinBlock, 0, s>>>(a, ranges, partial);
         };
         auto with = [&](auto sum) {
             if constexpr (decltype(sum)::value && two_value_tiles(NP, sizeof(T))) {

@@ -73,6 +73,14 @@ __device__ inline int turned_x()
     return (int)((blockIdx.x + row * gridDim.x / kXcds) % gridDim.x);
 }
 
+// A grid of at least `blocks` workgroups of up to 256 threads on two axes: one axis holds fewer than 2^32 threads.
+inline dim3 grid_of(size_t blocks)
+{
+    constexpr size_t kMost = (size_t)1 << 22;
+    const size_t rows = (blocks + kMost - 1) / kMost;
+    return dim3((unsigned)((blocks + rows - 1) / rows), (unsigned)rows);
+}
+
 // The page of position `pos` of sequence b, or -1 where there is none.  pos may be anything.
 __host__ __device__ inline int page_of(const CacheView &c, int b, long pos)
 {

@@ -27,3 +27,7 @@ def build_and_run(tmp_path, *sources):
 
 def test_rows_of_a_diagonal(tmp_path):
     build_and_run(tmp_path, os.path.join(SAN, "diagonal_san.hip"))
+
+
+def test_grids(tmp_path):
+    build_and_run(tmp_path, os.path.join(SAN, "grid_san.hip"))
