@@ -373,7 +373,7 @@ spin_status spin_cache_compact(const spin_cache *c, int nodes, const int32_t *co
  * and everywhere else the public constant `masked` (party 0 holds it, the others 0).
  * Q, A: [n][batch][heads][nodes][dim]; C, r, r_top, r_msb, out: [n][batch][heads][nodes][columns].  Triples satisfy sum_i C_i = (sum A_i)(sum b_i)
  * with the masks that the rows were opened with.  tuple pointers are ignored when f = 0; out may alias C, and r, r_top or r_msb.
- * bias may be NULL; with it depth ([batch][nodes] or NULL: 0, 1, ..) is the distance of a node behind the context: its position is
+ * bias may be NULL (depth is then not looked at); with it depth ([batch][nodes] or NULL: 0, 1, ..) is the distance of a node behind the context: its position is
  * context[b] + depth[b][m] as query and as key.  heads is a multiple of c->heads; c->V is not looked at.  0 <= f <= 61.  Refused (SPIN_ERANGE), here
  * and below, are more than 2^24 columns and more than 65535 of heads * nodes, of batch * c->heads or, if f = 0, of batch * c->n (in spin_cache_values
  * over more than three columns, which refuses more than 32767 cached heads of more than 128 64-bit words as well).                    */

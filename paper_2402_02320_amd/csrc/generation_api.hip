@@ -92,7 +92,7 @@ spin_status attend(bool scores, const spin_cache *c, int heads, int nodes, int c
         const size_t need = cache_values_workspace(c->n, c->batch, heads, c->heads, nodes, columns, c->dim, sizeof(T));
         if (workspace == nullptr || ((uintptr_t)workspace & 255) != 0 || workspace_bytes < need) return SPIN_EWORKSPACE;
     }
-    AttentionArgs<T> a{view_of(*c), {nodes, columns, context, tree}, {0, 0, nullptr, nullptr}, depth, c->n, c->batch, heads, f, (const T *)pool, x, A, C,
+    AttentionArgs<T> a{view_of(*c), {nodes, columns, context, tree}, {0, 0, nullptr, nullptr}, bias ? depth : nullptr, c->n, c->batch, heads, f, (const T *)pool, x, A, C,
                        r, r_top, r_msb, masked, out, workspace};
     if (bias) a.bias = BiasView{bias->buckets, bias->reach, bias->bucket_of, bias->table};
     return scores ? launch_cache_scores<T>(a, (hipStream_t)stream) : launch_cache_values<T>(a, (hipStream_t)stream);

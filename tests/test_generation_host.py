@@ -31,3 +31,8 @@ def test_rows_of_a_diagonal(tmp_path):
 
 def test_grids(tmp_path):
     build_and_run(tmp_path, os.path.join(SAN, "grid_san.hip"))
+
+
+def test_what_the_launchers_are_given(tmp_path):
+    from paper_2402_02320_amd import build
+    build_and_run(tmp_path, os.path.join(build.CSRC, "generation_api.hip"), os.path.join(SAN, "dispatch_san.hip"))
