@@ -116,12 +116,15 @@ class ShareCache:
         for s, k in zip(sequences, kept):
             if self._length[s] < nodes or any(not 0 <= a < nodes for a in k) or any(a >= b for a, b in zip(k, k[1:])):
                 raise spin.SpinError("kept rows are ascending indices into the draft")
-        moved = [(s, self._length[s] - nodes + next(j for j, a in enumerate(k) if a != j), self._length[s] - nodes + len(k))
-                 for s, k in zip(sequences, kept) if list(k) != list(range(len(k)))]
-        self._own(moved)
-        if moved:
-            self.ring.cache_compact(self.pools, self.table(sequences), self.context(sequences, nodes), self._ints([list(k) + [0] * (nodes - len(k)) for k in kept]),
-                                    self._ints([len(k) for k in kept]))
+        moved = []                                         # (sequence, position of the first row that moves, the rows from there on)
+        for s, k in zip(sequences, kept):
+            j = next((j for j, a in enumerate(k) if a != j), None)
+            if j is not None:
+                moved.append((s, self._length[s] - nodes + j, [a - j for a in list(k)[j:]]))
+        self._own([(s, first, first + len(k)) for s, first, k in moved])
+        if moved:                                          # nothing else is handed over: what stays may be on pages that others have too
+            self.ring.cache_compact(self.pools, self.table([s for s, _, _ in moved]), self._ints([first for _, first, _ in moved]),
+                                    self._ints([k + [0] * (nodes - len(k)) for _, _, k in moved]), self._ints([len(k) for _, _, k in moved]))
         for s, k in zip(sequences, kept):
             self._length[s] += len(k) - nodes
             used = -(-self._length[s] // self.page_tokens)
