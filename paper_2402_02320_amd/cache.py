@@ -51,8 +51,9 @@ class ShareCache:
             if not self._refs[p]:
                 self._free.append(p)
 
-    def _own(self, wanted):
-        """Makes the pages of positions first to last - 1 of every (sequence, first, last) its own: new ones, or copies of shared ones.  All of them, or an error and nothing."""
+    def _write(self, wanted, call):
+        """Makes the pages of positions first to last - 1 of every (sequence, first, last) its own, new ones or copies of shared ones, and makes the call that writes
+        to them.  All of it, or an error, and every sequence has the pages that it had."""
         t, plan = self.page_tokens, []
         refs = dict()
         for s, first, last in wanted:
@@ -66,21 +67,32 @@ class ShareCache:
                 plan.append((s, k, p))
         if len(plan) > len(self._free):
             raise spin.SpinError("the cache is out of pages: %d more are needed, %d are left" % (len(plan), len(self._free)))
-        src, dst = [], []
+        taken = []                                         # (sequence, which of its pages, the page before or None, its own)
         for s, k, p in plan:
             q = self._free.pop()
             self._refs[q] = 1
+            taken.append((s, k, p, q))
             if p is None:
                 assert k == len(self._pages[s])
                 self._pages[s].append(q)
-                continue
-            self._refs[p] -= 1
-            self._pages[s][k] = q
-            if k * t < self._length[s]:                    # something is in it
-                src.append(p)
-                dst.append(q)
-        if src:
-            self.ring.cache_copy(self.pools, self._ints(src), self._ints(dst))
+            else:
+                self._refs[p] -= 1
+                self._pages[s][k] = q
+        filled = [(p, q) for s, k, p, q in taken if p is not None and k * t < self._length[s]]         # something is in it
+        try:
+            if filled:
+                self.ring.cache_copy(self.pools, self._ints([p for p, _ in filled]), self._ints([q for _, q in filled]))
+            call()
+        except BaseException:
+            for s, k, p, q in reversed(taken):
+                self._refs[q] = 0
+                self._free.append(q)
+                if p is None:
+                    self._pages[s].pop()
+                else:
+                    self._refs[p] += 1
+                    self._pages[s][k] = p
+            raise
 
     # ---- what the kernels read ------------------------------------------------------------------------------------
     def _ints(self, v):
@@ -104,8 +116,8 @@ class ShareCache:
         counts = [rows] * len(sequences) if counts is None else list(counts)
         if len(counts) != len(sequences) or any(not 0 <= c <= rows for c in counts):
             raise spin.SpinError("counts: one for every sequence, none over the number of rows")
-        self._own([(s, self._length[s], self._length[s] + c) for s, c in zip(sequences, counts) if c])
-        self.ring.cache_append(self.pools, self.table(sequences), self.context(sequences), x, b, count=self._ints(counts))
+        self._write([(s, self._length[s], self._length[s] + c) for s, c in zip(sequences, counts) if c],
+                    lambda: self.ring.cache_append(self.pools, self.table(sequences), self.context(sequences), x, b, count=self._ints(counts)))
         for s, c in zip(sequences, counts):
             self._length[s] += c
 
@@ -121,10 +133,10 @@ class ShareCache:
             j = next((j for j, a in enumerate(k) if a != j), None)
             if j is not None:
                 moved.append((s, self._length[s] - nodes + j, [a - j for a in list(k)[j:]]))
-        self._own([(s, first, first + len(k)) for s, first, k in moved])
         if moved:                                          # nothing else is handed over: what stays may be on pages that others have too
-            self.ring.cache_compact(self.pools, self.table([s for s, _, _ in moved]), self._ints([first for _, first, _ in moved]),
-                                    self._ints([k + [0] * (nodes - len(k)) for _, _, k in moved]), self._ints([len(k) for _, _, k in moved]))
+            self._write([(s, first, first + len(k)) for s, first, k in moved],
+                        lambda: self.ring.cache_compact(self.pools, self.table([s for s, _, _ in moved]), self._ints([first for _, first, _ in moved]),
+                                                        self._ints([k + [0] * (nodes - len(k)) for _, _, k in moved]), self._ints([len(k) for _, _, k in moved])))
         for s, k in zip(sequences, kept):
             self._length[s] += len(k) - nodes
             used = -(-self._length[s] // self.page_tokens)
