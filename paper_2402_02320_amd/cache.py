@@ -8,6 +8,9 @@ import torch
 from . import spin
 
 
+_MOST_PAIRS = 65535                        # of one call of cache_copy
+
+
 class ShareCache:
     """n parties, pages of page_tokens positions, `heads` cached heads of `dim` elements; bits: the ring's."""
 
@@ -51,6 +54,12 @@ class ShareCache:
             if not self._refs[p]:
                 self._free.append(p)
 
+    def _copy(self, pairs):
+        """Copies pages (from, to), in as many calls as it takes: no page is written twice, or read and written."""
+        for k in range(0, len(pairs), _MOST_PAIRS):
+            src, dst = zip(*pairs[k:k + _MOST_PAIRS])
+            self.ring.cache_copy(self.pools, self._ints(src), self._ints(dst))
+
     def _write(self, wanted, call):
         """Makes the pages of positions first to last - 1 of every (sequence, first, last) its own, new ones or copies of shared ones, and makes the call that writes
         to them.  All of it, or an error, and every sequence has the pages that it had."""
@@ -81,7 +90,7 @@ class ShareCache:
         filled = [(p, q) for s, k, p, q in taken if p is not None and k * t < self._length[s]]         # something is in it
         try:
             if filled:
-                self.ring.cache_copy(self.pools, self._ints([p for p, _ in filled]), self._ints([q for _, q in filled]))
+                self._copy(filled)
             call()
         except BaseException:
             for s, k, p, q in reversed(taken):
@@ -149,7 +158,7 @@ class ShareCache:
         low = [p for p in range(len(used)) if p not in used]
         moved = dict(zip(sorted(p for p in used if p >= len(used)), low))
         if moved:
-            self.ring.cache_copy(self.pools, self._ints(list(moved)), self._ints(list(moved.values())))
+            self._copy(list(moved.items()))
             for pages in self._pages.values():
                 pages[:] = [moved.get(p, p) for p in pages]
             for p, q in moved.items():
