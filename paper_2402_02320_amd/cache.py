@@ -135,7 +135,7 @@ class ShareCache:
         if len(set(sequences)) < len(sequences) or len(kept) != len(sequences):
             raise spin.SpinError("a list of kept rows for every sequence, once")
         for s, k in zip(sequences, kept):
-            if self._length[s] < nodes or any(not 0 <= a < nodes for a in k) or any(a >= b for a, b in zip(k, k[1:])):
+            if not 0 <= nodes <= self._length[s] or any(not 0 <= a < nodes for a in k) or any(a >= b for a, b in zip(k, k[1:])):
                 raise spin.SpinError("kept rows are ascending indices into the draft")
         moved = []                                         # (sequence, position of the first row that moves, the rows from there on)
         for s, k in zip(sequences, kept):
