@@ -724,14 +724,21 @@ def _shapes(ok):
         raise SpinError("inconsistent operand shapes")
 
 
+def _ints(*values):
+    """The numbers, each of which the library takes as an int; ctypes hands on the low half of a larger one."""
+    if any(not -2 ** 31 <= v < 2 ** 31 for v in values):
+        raise SpinError("a number or a length does not fit an int")
+    return values
+
+
 def _cache(word, K, V, table, batch):
     """The library's description of a cache, of one pool where the other is None."""
     pool = V if K is None else K
     _shapes(pool.dim() == 5 and (K is None or V is None or V.shape == K.shape))
-    slots, pages, heads, tokens, dim = pool.shape
+    slots, pages, heads, tokens, dim = _ints(*pool.shape)
     at = None if table is None else _list32(table, "table", batch, None)
     return _Cache(slots - 1, pages, heads, tokens, dim, None if K is None else word.dev(K, "K"), None if V is None else word.dev(V, "V"),
-                  batch, 0 if table is None else table.shape[1], at)
+                  *_ints(batch, 0 if table is None else table.shape[1]), at)
 
 
 def _bias(word, bias, n, heads):
@@ -743,7 +750,7 @@ def _bias(word, bias, n, heads):
 def _bucketing(bucket_of, buckets, table=None):
     if bucket_of.numel() % 2 == 0:
         raise SpinError("bucket_of has an entry for each distance from -reach to reach")
-    return _RelBias(buckets, bucket_of.numel() // 2, _list32(bucket_of, "bucket_of", None), table)
+    return _RelBias(*_ints(buckets, bucket_of.numel() // 2), _list32(bucket_of, "bucket_of", None), table)
 
 
 def _tuple_ptrs(word, tuple_, f, shape):
@@ -780,7 +787,7 @@ class _Word:
                 return _done(done)
         (K, V), (Kx, Vx), (Kb, Vb) = pools, x, b
         _shapes(Kx.dim() == 5 and all(t.shape == Kx.shape for t in (Vx, Kb, Vb)))
-        n, batch, heads, rows, dim = Kx.shape
+        n, batch, heads, rows, dim = _ints(*Kx.shape)
         c = _cache(self, K, V, table, batch)
         _shapes((c.n, c.heads, c.dim) == (n, heads, dim))
         _check(self.entry("cache_append")(ctypes.byref(c), rows, _list32(start, "start", batch), None if count is None else _list32(count, "count", batch),
@@ -794,7 +801,7 @@ class _Word:
             if done is not None:
                 return _done(done)
         c = _cache(self, pools[0], pools[1], None, 0)
-        _check(self.entry("cache_copy")(ctypes.byref(c), src.numel(), _list32(src, "src", None), _list32(dst, "dst", src.numel()), _stream()))
+        _check(self.entry("cache_copy")(ctypes.byref(c), *_ints(src.numel()), _list32(src, "src", None), _list32(dst, "dst", src.numel()), _stream()))
         return pools
 
     def cache_compact(self, pools, table, context, kept, kept_count):
@@ -805,7 +812,7 @@ class _Word:
             if done is not None:
                 return _done(done)
         _shapes(kept.dim() == 2)
-        batch, nodes = kept.shape
+        batch, nodes = _ints(*kept.shape)
         c = _cache(self, pools[0], pools[1], table, batch)
         _check(self.entry("cache_compact")(ctypes.byref(c), nodes, _list32(context, "context", batch), _list32(kept, "kept", batch, nodes),
                                            _list32(kept_count, "kept_count", batch), _stream()))
@@ -830,13 +837,13 @@ class _Word:
             if done is not None:
                 return _done(done)
         _shapes(Q.dim() == 5 and A.shape == Q.shape and C.dim() == 5 and C.shape[:4] == Q.shape[:4])
-        n, batch, heads, nodes, dim = Q.shape
+        n, batch, heads, nodes, dim, columns, f = _ints(*Q.shape, C.shape[4], f)
         c = _cache(self, K, None, table, batch)
         _shapes((c.n, c.dim) == (n, dim))
         r, r_top, r_msb = _tuple_ptrs(self, tuple_, f, C.shape)
         if out is None:
             out = torch.empty_like(C)
-        _check(self.entry("cache_scores")(ctypes.byref(c), heads, nodes, C.shape[4], f, _list32(context, "context", batch), self._tree(tree, batch, nodes),
+        _check(self.entry("cache_scores")(ctypes.byref(c), heads, nodes, columns, f, _list32(context, "context", batch), self._tree(tree, batch, nodes),
                                           self.dev(Q, "Q"), self.dev(A, "A"), self.dev(C, "C"), r, r_top, r_msb, masked % (1 << self.bits),
                                           None if bias is None else ctypes.byref(_bias(self, bias, n, heads)),
                                           None if bias is None or depth is None else _list32(depth, "depth", batch, nodes),
@@ -844,8 +851,8 @@ class _Word:
         return out
 
     def cache_values_workspace_bytes(self, V, table, heads, nodes, columns):
-        slots, pages, cached, tokens, dim = V.shape
-        c = _Cache(slots - 1, pages, cached, tokens, dim, None, None, table.shape[0], table.shape[1], table.data_ptr())
+        slots, pages, cached, tokens, dim, heads, nodes, columns = _ints(*V.shape, heads, nodes, columns)
+        c = _Cache(slots - 1, pages, cached, tokens, dim, None, None, *_ints(*table.shape[:2]), table.data_ptr())
         return int(self.entry("cache_values_workspace_bytes")(ctypes.byref(c), heads, nodes, columns))
 
     def cache_values(self, V, table, context, P, A, C, f=0, tuple_=None, tree=None, out=None, workspace=None):
@@ -856,7 +863,7 @@ class _Word:
             if done is not None:
                 return _done(done)
         _shapes(P.dim() == 5 and A.shape == P.shape and C.dim() == 5 and C.shape[:4] == P.shape[:4])
-        n, batch, heads, nodes, columns = P.shape
+        n, batch, heads, nodes, columns, f = _ints(*P.shape, f)
         c = _cache(self, None, V, table, batch)
         _shapes((c.n, c.dim) == (n, C.shape[4]))
         r, r_top, r_msb = _tuple_ptrs(self, tuple_, f, C.shape)
@@ -880,7 +887,7 @@ class _Word:
             if done is not None:
                 return _done(done)
         _shapes(x.dim() == 5)
-        n, batch, heads, Q, K = x.shape
+        n, batch, heads, Q, K, first, f = _ints(*x.shape, first, f)
         v = _bias(self, (bias, bucket_of), n, heads)
         r, r_top, r_msb = _tuple_ptrs(self, tuple_, f, x.shape)
         if out is None:
@@ -896,7 +903,7 @@ class _Word:
             if done is not None:
                 return _done(done)
         _shapes(dS.dim() == 5)
-        n, batch, heads, Q, K = dS.shape
+        n, batch, heads, Q, K, first = _ints(*dS.shape, first)
         v = _bucketing(bucket_of, buckets)
         if out is None:
             out = torch.empty((n, heads, buckets), dtype=dS.dtype, device=dS.device)
