@@ -1,7 +1,8 @@
 """Which page of a paged cache holds what: sequences that grow, fork, are cut back to an accepted draft and end, over the pools that spin.cache_append,
 cache_copy, cache_compact, cache_scores and cache_values work on.
 
-All bookkeeping is on the host; only the tables, lengths and page lists that the kernels read go to the device, with each call.  Pages are handed on as soon as nothing refers to them,
+All bookkeeping is on the host; only the tables, lengths and page lists that the kernels read go to the device, with each call, by copies that the host waits for: none of these calls
+can be captured into a graph.  Pages are handed on as soon as nothing refers to them,
 so all calls on one cache belong on one stream (or are ordered otherwise)."""
 import torch
 
