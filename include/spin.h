@@ -8,8 +8,10 @@
  * a public linear combination with fused truncation, and for generating token by
  * token a paged cache of shared keys and values, the attention products of a tree
  * of drafted tokens over it and a relative position bias (spin_cache_*,
- * spin_relbias_*).  Measurement aids (per-kernel event timing, an MFMA rate
- * probe) are declared in spin_bench.h.
+ * spin_relbias_*), and for blocks without softmax linear attention with a decay
+ * and layer norm, forward and backward (spin_linattn_*, spin_layernorm*).
+ * Measurement aids (per-kernel event timing, an MFMA rate probe) are declared
+ * in spin_bench.h.
  *
  * Conventions that hold for every entry point
  * -------------------------------------------
@@ -427,6 +429,124 @@ spin_status spin32_relbias_trunc(int n, int batch, int heads, int Q, int K, int 
                                  uint32_t masked, const spin_relbias *bias, uint32_t *out, spin_stream stream);
 spin_status spin32_relbias_grad(int n, int batch, int heads, int Q, int K, int first, int causal, const int32_t *lengths,
                                 const uint32_t *dS, const spin_relbias *bias, uint32_t *grad, spin_stream stream);
+
+/* ---- Linear attention with a decay, and layer norm ----------------------------------------------------
+ * What a transformer block without softmax multiplies.  A secret x is opened once, E = sum_i (x_i - a_i) against the mask a dealt for it, and
+ * every product with it takes the same E: beside the dealt share C_i of the masks' product party i adds E . b_i + a_i . F, and party 0 E . F.  T(z, f)
+ * is the truncation of spin_trunc by f bits.  Entry points spin32_* take the same structures over arrays of uint32_t.                          */
+typedef struct { const void *value, *mask; } spin_masked;          /* shares and the masks that they are opened against, of one shape */
+typedef struct { const void *r, *r_top, *r_msb; } spin_tuple;      /* a truncation tuple, of the result's shape                       */
+
+/* Linear attention takes `tokens` in chunks of `chunk`, the last of them cut; chunks = ceil(tokens / chunk).  A head's decay is public: w[j] is
+ * round(lambda^j 2^g).  Sequence b has lengths[b] tokens (at most `tokens`; below zero counts as none), L of which are in the chunk at hand; what stands behind
+ * them is not looked at.  lengths is a device array of int32_t (4-byte aligned).                                             */
+typedef struct {
+    int n, batch, heads;
+    int tokens;
+    int chunk;               /* 32, 64 or 128                                                                        */
+    int f, g;                /* fractional bits of the factors (1 or more) and of w (0 or more), f + g <= 61 (29)    */
+    const void *decay;       /* device, [heads][chunk + 1] public ring words w, or NULL: all 1, and g is 0           */
+    const int32_t *lengths;  /* [batch], or NULL: all have `tokens`                                                  */
+} spin_linattn;
+
+/* Scores within a chunk, for j <= i < L of its tokens:   out[i][j] = T(C[i][j] + w[i - j] x_i . y_j, f + g),   0 elsewhere.
+ * x, y: [n][batch][heads][tokens][dim]; C, t, out: [n][batch][heads][chunks][chunk][chunk]; the masks satisfy sum C = w[i - j] (sum a_i . sum b_j).
+ * out may alias C or an array of t.  dim here, and rows and columns below, are multiples of 8 from 8 to 256.  Attention takes them of queries and keys; the gradient of
+ * the scores, of the result's gradient and the values.                                                                      */
+spin_status spin_linattn_scores(const spin_linattn *s, int dim, const spin_masked *x, const spin_masked *y, const uint64_t *C,
+                                const spin_tuple *t, uint64_t *out, spin_stream stream);
+
+/* States from chunk to chunk.  states[c] is the state S before chunk c is taken, `last` the one behind all; S begins as `first` (NULL: zeros), and a chunk
+ * with L > 0 tokens makes    S <- T(C[c] + 2^f w[L] S + sum_j w[L - 1 - j] x_j (x) y_j, f + g);   one without leaves it.
+ * reverse != 0 takes the chunks from the last to the first and weighs by w[j + 1]: the gradient of the states, of queries and the result's gradient; states[c] is then
+ * the gradient of what chunk c leaves, `last` that of `first`.  x: [n][batch][heads][tokens][rows]; y: [..][tokens][columns]; C, t, states:
+ * [n][batch][heads][chunks][rows][columns]; first, last: [n][batch][heads][rows][columns].  sum C = sum_j w (sum a_j) (x) (sum b_j).  states may alias C or an array
+ * of t, last may alias first.  workspace: device scratch of spin_linattn_states_workspace_bytes() bytes (0 if the arguments are invalid), 256-byte aligned.     */
+spin_status spin_linattn_states(const spin_linattn *s, int rows, int columns, int reverse, const spin_masked *x, const spin_masked *y,
+                                const uint64_t *C, const spin_tuple *t, const uint64_t *first, uint64_t *states, uint64_t *last,
+                                void *workspace, size_t workspace_bytes, spin_stream stream);
+size_t spin_linattn_states_workspace_bytes(const spin_linattn *s, int rows, int columns);
+
+/* Rows i < L of every chunk:    out_i = T(C_i + 2^g sum_j P_ij y_j + w[i + 1] x_i . S, f + g),    j <= i;   0 behind them.
+ * reverse != 0 takes P_ji, i <= j < L, and w[L - 1 - i].  P and its mask count as zero where no score is, whatever they hold there.
+ * P: [n][batch][heads][chunks][chunk][chunk]; y, C, t, out: [n][batch][heads][tokens][columns]; x: [..][tokens][rows]; S: [n][batch][heads][chunks][rows][columns],
+ * or [columns][rows] last where transposed != 0.  sum C is the same expression in the masks.  out may alias C or an array of t.  With the scores P of (Q, K), dP of (dO, V), the
+ * states S of (K, V), their gradients dS of (Q, dO):   O: (P, V, Q, S);   dQ: (dP, K, dO, S transposed);   dK: (dP, Q, V, dS transposed) reverse;
+ * dV: (P, dO, K, dS) reverse.                                                                                               */
+spin_status spin_linattn_outputs(const spin_linattn *s, int rows, int columns, int reverse, int transposed, const spin_masked *P,
+                                 const spin_masked *y, const spin_masked *x, const spin_masked *S, const uint64_t *C, const spin_tuple *t,
+                                 uint64_t *out, spin_stream stream);
+
+/* One token of every sequence b with active[b] > 0 (active NULL: all):   S' = T(CS + 2^f w[1] S + w[0] k (x) v, f + g),   out = T(CO + q . S', f),
+ * S' being opened against S_mask.  Of the others S' = S and out = 0.  s->tokens and s->chunk are not looked at, s->lengths is `active`, and decay is [heads][2].
+ * q, k: [n][batch][heads][rows]; v, CO, tO, out: [n][batch][heads][columns]; S, S_mask, CS, tS, S_out: [n][batch][heads][rows][columns].  S_out may alias S, S_mask, CS or
+ * an array of tS; out CO or an array of tO.                                                                                 */
+spin_status spin_linattn_step(const spin_linattn *s, int rows, int columns, const uint64_t *S, const spin_masked *q, const spin_masked *k,
+                              const spin_masked *v, const uint64_t *S_mask, const uint64_t *CS, const spin_tuple *tS, const uint64_t *CO,
+                              const spin_tuple *tO, uint64_t *S_out, uint64_t *out, spin_stream stream);
+
+/* Layer norm of rows of `dim` words at f fractional bits.  Means are sums times inv = (2^shift + dim / 2) / dim, truncated by `shift`: the larger the
+ * more exact, as long as a sum of dim words times inv stays in the ring.  dim: 1 to 8192.                                   */
+typedef struct {
+    int n, rows, dim;
+    int f;                   /* 1 to 60 (28)                                                                         */
+    int shift;               /* 1 to 61 (29)                                                                         */
+} spin_norm;
+
+/* Forward.  row_words [n][15 (iterations + 1)][rows] holds, a row of words each, what belongs to whole rows; t(k) are its words k, k + 1, k + 2 as a tuple:
+ *     mu  = T(inv sum x, shift), t(0);     xc = x - mu, opened against mask_x
+ *     q   = word 3 + sum xc^2;   v = T(inv T(q, f), shift) + [party 0] eps, t(4) and t(7);   y = T(2^f offset - slope v, f), t(10);   v is opened against word 13
+ *     for each iteration, k = 14, 29, ..:   y is opened against word k,  u = T(word k+1 + y y, f), t(k+2), against word k+5,
+ *         h = 3 2^f - T(word k+6 + u v, f), t(k+7), against word k+10,  y <- T(word k+11 + y h, f + 1), t(k+12)
+ *     rstd = y, opened against the last word;   xhat = T(C1 + xc rstd, f), t1, opened against mask_xhat;   out = T(C2 + xhat gamma, f) + beta, t2
+ * so 1 / sqrt(v) is Newton's, from the public line offset - slope v (ring words at f bits); it converges where that first guess y has 0 < v y^2 < 3.
+ * The words 3, k+1, k+6, k+11 and C1, C2 are the dealt shares of the masks' products.  x, mask_x, mask_xhat, C1, C2, t1, t2, out, xhat: [n][rows][dim]; gamma, beta:
+ * [n][dim]; rstd: [n][rows].  xhat and rstd, which the gradient takes, may be NULL.  out may alias C2 or an array of t2, xhat C1 or one of t1.
+ * 0 <= iterations <= 64.  workspace: device scratch of spin_layernorm_workspace_bytes() bytes (0 if the arguments are invalid), 256-byte aligned.     */
+#define SPIN_MAX_NORM_ITERATIONS 64
+spin_status spin_layernorm(const spin_norm *s, int iterations, uint64_t offset, uint64_t slope, uint64_t eps, const uint64_t *x,
+                           const spin_masked *gamma, const uint64_t *beta, const uint64_t *mask_x, const uint64_t *mask_xhat,
+                           const uint64_t *C1, const spin_tuple *t1, const uint64_t *C2, const spin_tuple *t2, const uint64_t *row_words,
+                           uint64_t *out, uint64_t *xhat, uint64_t *rstd, void *workspace, size_t workspace_bytes, spin_stream stream);
+size_t spin_layernorm_workspace_bytes(const spin_norm *s);
+
+/* Gradients from dy, that of the result.  column_words: [n][4][dim]; row_words: [n][22][rows], t(k) as above:
+ *     g      = T(C1 + dy gamma, f), t1;   dy, xhat and g are opened against their masks
+ *     dgamma = T(column word 0 + sum_rows dy xhat, f), column words 1 to 3;     dbeta = sum_rows dy
+ *     m1 = T(inv sum g, shift), t(0);   m2 = T(inv T(word 3 + sum g xhat, f), shift), t(4) and t(7);   rstd is opened against word 10
+ *     k1 = T(word 12 + m1 rstd, f), m1 against word 11, t(13);   k2 = T(word 17 + m2 rstd, f), m2 against word 16, t(18);   k2 is opened against word 21
+ *     dx = T(C2 + g rstd - xhat k2, f) - k1, t2
+ * Column word 0, words 3, 12, 17 and C1, C2 (of g rstd - xhat k2) are the dealt shares of the masks' products.  dy, xhat, C1, C2, t1, t2, dx: [n][rows][dim]; gamma, dgamma,
+ * dbeta: [n][dim]; rstd: [n][rows].  xhat's mask may be the forward pass's.  dx may alias C2 or an array of t2.  workspace as above.                              */
+spin_status spin_layernorm_grad(const spin_norm *s, const spin_masked *dy, const spin_masked *xhat, const uint64_t *rstd, const spin_masked *gamma,
+                                const uint64_t *mask_g, const uint64_t *C1, const spin_tuple *t1, const uint64_t *C2, const spin_tuple *t2,
+                                const uint64_t *row_words, const uint64_t *column_words, uint64_t *dx, uint64_t *dgamma, uint64_t *dbeta,
+                                void *workspace, size_t workspace_bytes, spin_stream stream);
+size_t spin_layernorm_grad_workspace_bytes(const spin_norm *s);
+
+/* The same over Z_2^32.                                                                                                          */
+spin_status spin32_linattn_scores(const spin_linattn *s, int dim, const spin_masked *x, const spin_masked *y, const uint32_t *C,
+                                const spin_tuple *t, uint32_t *out, spin_stream stream);
+spin_status spin32_linattn_states(const spin_linattn *s, int rows, int columns, int reverse, const spin_masked *x, const spin_masked *y,
+                                const uint32_t *C, const spin_tuple *t, const uint32_t *first, uint32_t *states, uint32_t *last,
+                                void *workspace, size_t workspace_bytes, spin_stream stream);
+size_t spin32_linattn_states_workspace_bytes(const spin_linattn *s, int rows, int columns);
+spin_status spin32_linattn_outputs(const spin_linattn *s, int rows, int columns, int reverse, int transposed, const spin_masked *P,
+                                 const spin_masked *y, const spin_masked *x, const spin_masked *S, const uint32_t *C, const spin_tuple *t,
+                                 uint32_t *out, spin_stream stream);
+spin_status spin32_linattn_step(const spin_linattn *s, int rows, int columns, const uint32_t *S, const spin_masked *q, const spin_masked *k,
+                              const spin_masked *v, const uint32_t *S_mask, const uint32_t *CS, const spin_tuple *tS, const uint32_t *CO,
+                              const spin_tuple *tO, uint32_t *S_out, uint32_t *out, spin_stream stream);
+spin_status spin32_layernorm(const spin_norm *s, int iterations, uint32_t offset, uint32_t slope, uint32_t eps, const uint32_t *x,
+                           const spin_masked *gamma, const uint32_t *beta, const uint32_t *mask_x, const uint32_t *mask_xhat,
+                           const uint32_t *C1, const spin_tuple *t1, const uint32_t *C2, const spin_tuple *t2, const uint32_t *row_words,
+                           uint32_t *out, uint32_t *xhat, uint32_t *rstd, void *workspace, size_t workspace_bytes, spin_stream stream);
+size_t spin32_layernorm_workspace_bytes(const spin_norm *s);
+spin_status spin32_layernorm_grad(const spin_norm *s, const spin_masked *dy, const spin_masked *xhat, const uint32_t *rstd, const spin_masked *gamma,
+                                const uint32_t *mask_g, const uint32_t *C1, const spin_tuple *t1, const uint32_t *C2, const spin_tuple *t2,
+                                const uint32_t *row_words, const uint32_t *column_words, uint32_t *dx, uint32_t *dgamma, uint32_t *dbeta,
+                                void *workspace, size_t workspace_bytes, spin_stream stream);
+size_t spin32_layernorm_grad_workspace_bytes(const spin_norm *s);
 
 /* Static description of a status code. */
 const char *spin_status_string(int status);

@@ -45,7 +45,9 @@ typedef enum {
     SPIN_KERNEL_CACHE = 16,          /* spin_cache_append, _copy, _compact */
     SPIN_KERNEL_ATTENTION = 17,      /* spin_cache_scores, _values */
     SPIN_KERNEL_RELBIAS = 18,        /* spin_relbias_trunc, _grad */
-    SPIN_KERNEL_COUNT = 19
+    SPIN_KERNEL_LINATTN = 19,        /* spin_linattn_* */
+    SPIN_KERNEL_LAYERNORM = 20,      /* spin_layernorm, _grad */
+    SPIN_KERNEL_COUNT = 21
 } spin_kernel;
 void spin_profile_enable(int on);
 spin_status spin_profile_read(int kernel, double *total_ms, unsigned *launches);

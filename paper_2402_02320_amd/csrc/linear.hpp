@@ -1,0 +1,99 @@
+// What the kernels of linear attention and layer norm share: their arguments as kernels see them.  Interface: spin_linattn_* and spin_layernorm* in
+// include/spin.h.
+#pragma once
+#include "generation.hpp"
+
+namespace spin {
+
+template <class T> struct Masked { const T *x, *a; };
+template <class T> struct Tuple { const T *r, *r_top, *r_msb; };
+
+struct ChunkView {                     // tokens and their chunks
+    int n, batch, heads, tokens, chunk, chunks, f, g;
+    const int32_t *lengths;
+};
+// A product of rows within chunks: scores, and (P null) the states' sums.
+template <class T> struct ScoresArgs {
+    ChunkView c;
+    const T *decay;
+    int dim;
+    Masked<T> x, y;
+    const T *C;
+    Tuple<T> t;
+    T *out;
+};
+template <class T> struct StatesArgs {
+    ChunkView c;
+    const T *decay;
+    int rows, columns;
+    bool reverse;
+    Masked<T> x, y;
+    const T *C;
+    Tuple<T> t;
+    const T *first;
+    T *states, *last, *opened;         // opened: workspace, a word an element of states
+};
+template <class T> struct OutputsArgs {
+    ChunkView c;
+    const T *decay;
+    int rows, columns;
+    bool reverse, transposed;
+    Masked<T> P, y, x, S;
+    const T *C;
+    Tuple<T> t;
+    T *out;
+};
+template <class T> struct StepArgs {
+    int n, batch, heads, f, g, rows, columns;
+    const T *decay;
+    const int32_t *active;
+    const T *S, *S_mask, *CS, *CO;
+    Masked<T> q, k, v;
+    Tuple<T> tS, tO;
+    T *S_out, *out;
+};
+template <class T> struct NormArgs {
+    int n, rows, dim, f, shift, iterations;
+    T inv, offset, slope, eps;
+    const T *x, *beta, *C1, *C2, *row_words;
+    const T *mask_x, *mask_xhat;
+    Masked<T> gamma;
+    Tuple<T> t1, t2;
+    T *out, *xhat, *rstd;
+    void *workspace;
+};
+template <class T> struct NormGradArgs {
+    int n, rows, dim, f, shift;
+    T inv;
+    Masked<T> dy, xhat, gamma;
+    const T *rstd, *mask_g, *C1, *C2, *row_words, *column_words;
+    Tuple<T> t1, t2;
+    T *dx, *dgamma, *dbeta;
+    void *workspace;
+};
+
+// T = u32 or u64
+template <class T> spin_status launch_linattn_scores(const ScoresArgs<T> &a, hipStream_t s);
+template <class T> spin_status launch_linattn_states(const StatesArgs<T> &a, hipStream_t s);
+template <class T> spin_status launch_linattn_outputs(const OutputsArgs<T> &a, hipStream_t s);
+template <class T> spin_status launch_linattn_step(const StepArgs<T> &a, hipStream_t s);
+template <class T> spin_status launch_layernorm(const NormArgs<T> &a, hipStream_t s);
+template <class T> spin_status launch_layernorm_grad(const NormGradArgs<T> &a, hipStream_t s);
+size_t layernorm_workspace(int n, int rows, int dim, int word_bytes);
+size_t layernorm_grad_workspace(int n, int rows, int dim, int word_bytes);
+
+constexpr int kNormWords = 15, kNormGradWords = 22;        // of a row: a Newton step's (and as many besides), the gradient's
+constexpr int kMostDim = 8192;
+
+namespace {
+
+// Tokens of sequence b that are in a chunk.
+__host__ __device__ inline int tokens_in(const ChunkView &c, int b, int chunk)
+{
+    const int length = c.lengths ? c.lengths[b] : c.tokens, all = length < c.tokens ? length : c.tokens;
+    const int left = all - chunk * c.chunk;                // chunk * c.chunk < c.tokens
+    return left < 0 ? 0 : left < c.chunk ? left : c.chunk;
+}
+
+}  // namespace
+}  // namespace spin

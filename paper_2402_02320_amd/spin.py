@@ -111,6 +111,12 @@ def lib():
                                    ("relbias_trunc", [i32] * 7 + [p, i32] + [p] * 4 + [word] + [p] * 3), ("relbias_grad", [i32] * 7 + [p] * 5)):
                 getattr(L, pre + name).argtypes = argtypes
                 getattr(L, pre + name).restype = sz if name.endswith("_bytes") else i32
+            for name, argtypes in (("linattn_scores", [p, i32] + [p] * 6), ("linattn_states", [p] + [i32] * 3 + [p] * 8 + [sz, p]),
+                                   ("linattn_states_workspace_bytes", [p, i32, i32]), ("linattn_outputs", [p] + [i32] * 4 + [p] * 8),
+                                   ("linattn_step", [p, i32, i32] + [p] * 12), ("layernorm", [p, i32] + [word] * 3 + [p] * 14 + [sz, p]),
+                                   ("layernorm_grad", [p] * 16 + [sz, p]), ("layernorm_workspace_bytes", [p]), ("layernorm_grad_workspace_bytes", [p])):
+                getattr(L, pre + name).argtypes = argtypes
+                getattr(L, pre + name).restype = sz if name.endswith("_bytes") else i32
         L.spin_probe_mfma.argtypes = [p, i32, i32, p, p]
         L.spin_probe_mfma.restype = i32
         L.spin_status_string.argtypes = [i32]
@@ -710,6 +716,28 @@ class _RelBias(ctypes.Structure):
     _fields_ = [("buckets", ctypes.c_int), ("reach", ctypes.c_int), ("bucket_of", ctypes.c_void_p), ("table", ctypes.c_void_p)]
 
 
+class _Masked(ctypes.Structure):
+    _fields_ = [("value", ctypes.c_void_p), ("mask", ctypes.c_void_p)]
+
+
+class _Tuple(ctypes.Structure):
+    _fields_ = [(k, ctypes.c_void_p) for k in ("r", "r_top", "r_msb")]
+
+
+class _LinAttn(ctypes.Structure):
+    _fields_ = [(k, ctypes.c_int) for k in ("n", "batch", "heads", "tokens", "chunk", "f", "g")] + [("decay", ctypes.c_void_p), ("lengths", ctypes.c_void_p)]
+
+
+class _Norm(ctypes.Structure):
+    _fields_ = [(k, ctypes.c_int) for k in ("n", "rows", "dim", "f", "shift")]
+
+
+def _on_this_device(t, name):
+    """Kernels run on the current device and its current stream: a tensor of another one is refused."""
+    if t.is_cuda and t.get_device() != torch.cuda.current_device():
+        raise SpinError("%s is on device %d, the current one is %d" % (name, t.get_device(), torch.cuda.current_device()))
+
+
 def _list32(t, name, *shape):
     """A device array of int32_t; its shape is checked as far as it is given (None: any length)."""
     if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype == torch.int32 and t.is_contiguous()):
@@ -912,7 +940,166 @@ class _Word:
         return out
 
 
-_CALLS_BY_WORD = ("cache_append", "cache_copy", "cache_compact", "cache_scores", "cache_values", "cache_values_workspace_bytes", "relbias_trunc", "relbias_grad")
+    # ---- linear attention with a decay, layer norm ----
+    def _masked(self, pair, name, *shape):
+        """(shares, masks) of that shape, as the library takes them."""
+        value, mask = pair
+        _shapes(tuple(value.shape) == shape and tuple(mask.shape) == shape)
+        return ctypes.byref(_Masked(self._of(value, name), self._of(mask, name)))
+
+    def _tuple(self, tuple_, *shape):
+        r = tuple(tuple_)
+        _shapes(len(r) == 3 and all(tuple(t.shape) == shape for t in r))
+        return ctypes.byref(_Tuple(*[self._of(t, k) for t, k in zip(r, ("r", "r_top", "r_msb"))]))
+
+    def _of(self, t, name, *shape):
+        """The address of a ring tensor (of that shape, if one is given) on the current device."""
+        if shape:
+            _shapes(tuple(t.shape) == shape)
+        _on_this_device(t, name)
+        return self.dev(t, name)
+
+    def _to(self, t, name, words):
+        _on_this_device(t, name)
+        return self.out(t, name, words)
+
+    def _heads(self, n, batch, heads, tokens, chunk, f, decay, g, lengths, name):
+        """The library's description of the heads and their chunks."""
+        if decay is None and g:
+            raise SpinError("without a decay there are no fractional bits g of it")
+        for t in (decay, lengths):
+            if t is not None:
+                _on_this_device(t, name)
+        return ctypes.byref(_LinAttn(*_ints(n, batch, heads, tokens, chunk, f, g), None if decay is None else self._of(decay, "decay", heads, chunk + 1),
+                                     None if lengths is None else _list32(lengths, name, batch)))
+
+    def linattn_scores(self, x, y, C, tuple_, f, decay=None, g=0, lengths=None, out=None):
+        """Scores of linear attention within chunks, T(C[i, j] + w[i - j] x_i . y_j, f + g) for tokens j <= i of a chunk that are there, else zero.
+        x, y: (shares, masks), [n, batch, heads, tokens, dim]; C, the truncation tuple and the result: [n, batch, heads, chunks, chunk, chunk], which says how long a chunk
+        is (32, 64 or 128).  decay: public words w [heads, chunk + 1], round(lambda^j 2^g), or None; lengths: tokens of every sequence, if not all."""
+        _shapes(x[0].dim() == 5 and C.dim() == 6)
+        n, batch, heads, tokens, dim, chunk = _ints(*x[0].shape, C.shape[5])
+        _shapes(chunk > 0)
+        pairs = (n, batch, heads, -(-tokens // chunk), chunk, chunk)
+        if out is None:
+            out = torch.empty_like(C)
+        _check(self.entry("linattn_scores")(self._heads(n, batch, heads, tokens, chunk, f, decay, g, lengths, "lengths"), dim,
+                                            self._masked(x, "x", n, batch, heads, tokens, dim), self._masked(y, "y", n, batch, heads, tokens, dim), self._of(C, "C", *pairs),
+                                            self._tuple(tuple_, *pairs), self._to(out, "out", C.numel()), _stream()))
+        return out
+
+    def linattn_states_workspace_bytes(self, n, batch, heads, tokens, chunk, rows, columns):
+        s = _LinAttn(*_ints(n, batch, heads, tokens, chunk, 1, 0), None, None)
+        return int(self.entry("linattn_states_workspace_bytes")(ctypes.byref(s), *_ints(rows, columns)))
+
+    def linattn_states(self, x, y, C, tuple_, f, chunk, decay=None, g=0, lengths=None, first=None, reverse=False, out=None, workspace=None):
+        """States of linear attention: (states, last), the state before every chunk and behind the last, from `first` (None: zeros) on.  A chunk of L > 0 tokens makes
+        S <- T(C + 2^f w[L] S + sum_j w[L - 1 - j] x_j (x) y_j, f + g).  reverse: chunks from the last, weights w[j + 1], as the gradient goes.
+        x, y: (shares, masks), [n, batch, heads, tokens, rows or columns]; C, the tuple and states: [n, batch, heads, chunks, rows, columns]; out: (states, last)."""
+        _shapes(x[0].dim() == 5 and y[0].dim() == 5)
+        n, batch, heads, tokens, rows, columns, chunk = _ints(*x[0].shape, y[0].shape[4], chunk)
+        _shapes(chunk > 0)
+        every, state = (n, batch, heads, -(-tokens // chunk), rows, columns), (n, batch, heads, rows, columns)
+        states, last = (torch.empty_like(C), C.new_empty(state)) if out is None else out
+        if workspace is None:
+            size = self.linattn_states_workspace_bytes(n, batch, heads, tokens, chunk, rows, columns)
+            if size == 0:
+                raise SpinError("invalid dimensions of linear attention")
+            workspace = torch.empty(size, dtype=torch.uint8, device=C.device)
+        _on_this_device(workspace, "workspace")
+        _check(self.entry("linattn_states")(self._heads(n, batch, heads, tokens, chunk, f, decay, g, lengths, "lengths"), rows, columns, 1 if reverse else 0,
+                                            self._masked(x, "x", n, batch, heads, tokens, rows), self._masked(y, "y", n, batch, heads, tokens, columns),
+                                            self._of(C, "C", *every), self._tuple(tuple_, *every), None if first is None else self._of(first, "first", *state),
+                                            self._to(states, "states", C.numel()), self._to(last, "last", n * batch * heads * rows * columns),
+                                            _workspace_ptr(workspace), workspace.numel() * workspace.element_size(), _stream()))
+        return states, last
+
+    def linattn_outputs(self, P, y, x, S, C, tuple_, f, decay=None, g=0, lengths=None, reverse=False, transposed=False, out=None):
+        """T(C_i + 2^g sum_{j <= i} P_ij y_j + w[i + 1] x_i . S, f + g) for the tokens i that are there, else zero; reverse: P_ji, i <= j, and w[L - 1 - i].
+        All factors are (shares, masks): P [n, batch, heads, chunks, chunk, chunk], y [n, batch, heads, tokens, columns], x [.., tokens, rows], S [.., chunks, rows, columns],
+        or [.., chunks, columns, rows] if transposed.  C, the tuple and the result: as y."""
+        _shapes(P[0].dim() == 6 and x[0].dim() == 5 and C.dim() == 5)
+        n, batch, heads, tokens, rows, columns, chunk = _ints(*x[0].shape, C.shape[4], P[0].shape[5])
+        _shapes(chunk > 0)
+        chunks, values = -(-tokens // chunk), (n, batch, heads, tokens, columns)
+        if out is None:
+            out = torch.empty_like(C)
+        _check(self.entry("linattn_outputs")(self._heads(n, batch, heads, tokens, chunk, f, decay, g, lengths, "lengths"), rows, columns, 1 if reverse else 0,
+                                             1 if transposed else 0, self._masked(P, "P", n, batch, heads, chunks, chunk, chunk), self._masked(y, "y", *values),
+                                             self._masked(x, "x", n, batch, heads, tokens, rows),
+                                             self._masked(S, "S", n, batch, heads, chunks, *((columns, rows) if transposed else (rows, columns))),
+                                             self._of(C, "C", *values), self._tuple(tuple_, *values), self._to(out, "out", C.numel()), _stream()))
+        return out
+
+    def linattn_step(self, S, q, k, v, mask, C, tuples, f, decay=None, g=0, active=None, out=None):
+        """One token of every sequence (with active[b] > 0, if given): (result, S'), S' = T(C[0] + 2^f w[1] S + w[0] k (x) v, f + g), result = T(C[1] + q . S', f).
+        The others keep their state and get zeros.  S, mask (of S'), C[0] and tuples[0]: [n, batch, heads, rows, columns]; q, k: (shares, masks), [n, batch, heads, rows]; v
+        likewise of columns, as C[1], tuples[1] and the result; decay: [heads, 2].  out: (result, S'), and S' may be S."""
+        _shapes(S.dim() == 5)
+        n, batch, heads, rows, columns = _ints(*S.shape)
+        state, value = tuple(S.shape), (n, batch, heads, columns)
+        result, after = (torch.empty_like(C[1]), torch.empty_like(S)) if out is None else out
+        _check(self.entry("linattn_step")(self._heads(n, batch, heads, 1, 1, f, decay, g, active, "active"), rows, columns, self._of(S, "S"),
+                                          self._masked(q, "q", n, batch, heads, rows), self._masked(k, "k", n, batch, heads, rows), self._masked(v, "v", *value),
+                                          self._of(mask, "mask", *state), self._of(C[0], "C", *state), self._tuple(tuples[0], *state), self._of(C[1], "C", *value),
+                                          self._tuple(tuples[1], *value), self._to(after, "S'", S.numel()), self._to(result, "out", n * batch * heads * columns), _stream()))
+        return result, after
+
+    def _norm(self, x, f, shift):
+        _shapes(x.dim() == 3)
+        return _Norm(*_ints(*x.shape, f, shift))
+
+    def _norm_workspace(self, name, s, workspace, device):
+        if workspace is None:
+            size = int(self.entry(name + "_workspace_bytes")(ctypes.byref(s)))
+            if size == 0:
+                raise SpinError("invalid dimensions of a layer norm")
+            workspace = torch.empty(size, dtype=torch.uint8, device=device)
+        _on_this_device(workspace, "workspace")
+        return workspace, _workspace_ptr(workspace), workspace.numel() * workspace.element_size()
+
+    def layernorm_workspace_bytes(self, n, rows, dim):
+        return int(self.entry("layernorm_workspace_bytes")(ctypes.byref(_Norm(*_ints(n, rows, dim, 1, 1)))))
+
+    def layernorm_grad_workspace_bytes(self, n, rows, dim):
+        return int(self.entry("layernorm_grad_workspace_bytes")(ctypes.byref(_Norm(*_ints(n, rows, dim, 1, 1)))))
+
+    def layernorm(self, x, gamma, beta, masks, C, tuples, row_words, f, shift, line, eps=0, out=None, workspace=None):
+        """Layer norm of rows x [n, rows, dim]: (result, xhat, rstd).  gamma: (shares, masks), [n, dim], as beta; masks, C, tuples: two each, of the centred rows and of
+        xhat, all as x; row_words: [n, 15 (iterations + 1), rows], in the order listed at spin_layernorm.  Means are sums times round(2^shift / dim), truncated by shift;
+        1 / sqrt(variance + eps) is Newton's from the public line (offset, slope), offset - slope * variance; eps, offset, slope: words at f bits."""
+        s = self._norm(x, f, shift)
+        n, rows, dim = shape = tuple(x.shape)
+        _shapes(row_words.dim() == 3 and row_words.shape[1] % 15 == 0 and row_words.shape[1] > 0)
+        result, xhat, rstd = (torch.empty_like(x), torch.empty_like(x), x.new_empty((n, rows))) if out is None else out
+        workspace, at, size = self._norm_workspace("layernorm", s, workspace, x.device)
+        offset, slope = line
+        _check(self.entry("layernorm")(ctypes.byref(s), row_words.shape[1] // 15 - 1, *[v % (1 << self.bits) for v in (offset, slope, eps)], self._of(x, "x"),
+                                       self._masked(gamma, "gamma", n, dim), self._of(beta, "beta", n, dim), self._of(masks[0], "mask", *shape),
+                                       self._of(masks[1], "mask", *shape), self._of(C[0], "C", *shape), self._tuple(tuples[0], *shape), self._of(C[1], "C", *shape),
+                                       self._tuple(tuples[1], *shape), self._of(row_words, "row_words", n, row_words.shape[1], rows),
+                                       self._to(result, "out", x.numel()), None if xhat is None else self._to(xhat, "xhat", x.numel()),
+                                       None if rstd is None else self._to(rstd, "rstd", n * rows), at, size, _stream()))
+        return result, xhat, rstd
+
+    def layernorm_grad(self, dy, xhat, rstd, gamma, masks, C, tuples, row_words, column_words, f, shift, out=None, workspace=None):
+        """Gradients (of x, gamma, beta) from dy, that of the result of layernorm, and its xhat and rstd.  masks: of dy, xhat and dy * gamma; C, tuples: two each, of
+        dy * gamma and of the gradient of x, all as dy [n, rows, dim]; row_words: [n, 22, rows], column_words: [n, 4, dim], as listed at spin_layernorm_grad."""
+        s = self._norm(dy, f, shift)
+        n, rows, dim = shape = tuple(dy.shape)
+        dx, dgamma, dbeta = (torch.empty_like(dy), dy.new_empty((n, dim)), dy.new_empty((n, dim))) if out is None else out
+        workspace, at, size = self._norm_workspace("layernorm_grad", s, workspace, dy.device)
+        _check(self.entry("layernorm_grad")(ctypes.byref(s), self._masked((dy, masks[0]), "dy", *shape), self._masked((xhat, masks[1]), "xhat", *shape),
+                                            self._of(rstd, "rstd", n, rows), self._masked(gamma, "gamma", n, dim), self._of(masks[2], "mask", *shape),
+                                            self._of(C[0], "C", *shape), self._tuple(tuples[0], *shape), self._of(C[1], "C", *shape), self._tuple(tuples[1], *shape),
+                                            self._of(row_words, "row_words", n, 22, rows), self._of(column_words, "column_words", n, 4, dim),
+                                            self._to(dx, "out", dy.numel()), self._to(dgamma, "out", n * dim), self._to(dbeta, "out", n * dim), at, size, _stream()))
+        return dx, dgamma, dbeta
+
+
+_CALLS_BY_WORD = ("cache_append", "cache_copy", "cache_compact", "cache_scores", "cache_values", "cache_values_workspace_bytes", "relbias_trunc", "relbias_grad",
+                  "linattn_scores", "linattn_states", "linattn_states_workspace_bytes", "linattn_outputs", "linattn_step",
+                  "layernorm", "layernorm_workspace_bytes", "layernorm_grad", "layernorm_grad_workspace_bytes")
 for _name in _CALLS_BY_WORD:
     globals()[_name] = getattr(_Word(64), _name)
     setattr(ring32, _name, staticmethod(getattr(_Word(32), _name)))
@@ -938,7 +1125,7 @@ def relative_buckets(buckets, reach, both_ways):
 
 KERNELS = {"random": 0, "share": 1, "open": 2, "beaver_mul": 3, "trunc": 4, "pack": 5, "gemm_limb": 6,
            "gemm_valu": 7, "lincomb": 8, "binary": 9, "cast": 10, "probe": 11, "beaver_mul_trunc": 12,
-           "gemm_residue": 13, "combine": 14, "gemm_direct": 15, "cache": 16, "attention": 17, "relbias": 18}
+           "gemm_residue": 13, "combine": 14, "gemm_direct": 15, "cache": 16, "attention": 17, "relbias": 18, "linattn": 19, "layernorm": 20}
 
 
 def probe_mfma(operands, blocks, iters, sink=None):
