@@ -502,8 +502,8 @@ typedef struct {
  * so 1 / sqrt(v) is Newton's, from the public line offset - slope v (ring words at f bits); it converges where that first guess y has 0 < v y^2 < 3.
  * The words 3, k+1, k+6, k+11 and C1, C2 are the dealt shares of the masks' products.  x, mask_x, mask_xhat, C1, C2, t1, t2, out, xhat: [n][rows][dim]; gamma, beta:
  * [n][dim]; rstd: [n][rows].  xhat and rstd, which the gradient takes, may be NULL.  out may alias C2 or an array of t2, xhat C1 or one of t1.
- * 0 <= iterations <= 64.  workspace: device scratch of spin_layernorm_workspace_bytes() bytes (0 if the arguments are invalid), 256-byte aligned.     */
-#define SPIN_MAX_NORM_ITERATIONS 64
+ * 0 <= iterations <= 16.  workspace: device scratch of spin_layernorm_workspace_bytes() bytes (0 if the arguments are invalid), 256-byte aligned.     */
+#define SPIN_MAX_NORM_ITERATIONS 16
 spin_status spin_layernorm(const spin_norm *s, int iterations, uint64_t offset, uint64_t slope, uint64_t eps, const uint64_t *x,
                            const spin_masked *gamma, const uint64_t *beta, const uint64_t *mask_x, const uint64_t *mask_xhat,
                            const uint64_t *C1, const spin_tuple *t1, const uint64_t *C2, const spin_tuple *t2, const uint64_t *row_words,

@@ -12,7 +12,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libspin.so")
 BINDING = os.path.join(HERE, "_binding.so")
 SOURCES = ["spin_api.hip", "elementwise.hip", "gemm_valu.hip", "gemm_limb.hip", "gemm_limb128.hip", "gemm_strassen.hip", "gemm_residue.hip", "gemm_direct.hip", "probe.hip",
-           "generation_api.hip", "cache.hip", "cache_attention.hip", "relbias.hip", "linear_api.hip", "linattn.hip", "layernorm.hip"]
+           "generation_api.hip", "cache.hip", "cache_attention.hip", "relbias.hip", "linear_api.hip", "linattn.hip", "layernorm.hip", "layernorm_grad.hip"]
 COMPILE_FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
                  "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
                  "-Wall", "-Wno-unused-command-line-argument"]

@@ -105,7 +105,9 @@ spin_status run_step(const spin_linattn *s, int rows, int columns, const T *S, c
 spin_status check_norm(const spin_norm *s, int most)
 {
     if (s == nullptr || bad_n(s->n) || s->rows < 1 || s->dim < 1 || s->dim > kMostDim || s->f < 1 || s->f >= most || s->shift < 1 || s->shift > most) return SPIN_EINVAL;
-    return s->rows > (1 << 24) || (double)s->n * s->rows * s->dim > kMaxWords ? SPIN_ERANGE : SPIN_OK;
+    // a launch has fewer than 2^32 threads
+    if (s->rows > (1 << 24) || (double)s->rows * norm_waves(s->dim) * 64 > (double)(1u << 31)) return SPIN_ERANGE;
+    return (double)s->n * s->rows * s->dim > kMaxWords ? SPIN_ERANGE : SPIN_OK;
 }
 
 template <class T> T inverse(const spin_norm &s) { return (T)((((uint64_t)1 << s.shift) + s.dim / 2) / s.dim); }

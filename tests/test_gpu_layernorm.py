@@ -21,7 +21,7 @@ CASES = {
     "eight_wide": (8, 3, 4100, 2),
     "five_parties": (5, 50, 257, 3),
     "many_rows": (2, 2500, 48, 2),
-    "below_a_wave": (4, 3, 63, 64),
+    "below_a_wave": (4, 3, 63, 16),
     "long_odd": (3, 11, 2049, 2),
     "six": (6, 4, 1025, 1),
     "seven": (7, 4, 129, 1),
