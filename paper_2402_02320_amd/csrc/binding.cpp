@@ -37,6 +37,15 @@ template <> struct ByWord<uint64_t> {
     decltype(&spin_cache_values_workspace_bytes) values_bytes;
     decltype(&spin_relbias_trunc) bias;
     decltype(&spin_relbias_grad) grad;
+    decltype(&spin_linattn_scores) linattn_scores;
+    decltype(&spin_linattn_states) linattn_states;
+    decltype(&spin_linattn_states_workspace_bytes) linattn_states_bytes;
+    decltype(&spin_linattn_outputs) linattn_outputs;
+    decltype(&spin_linattn_step) linattn_step;
+    decltype(&spin_layernorm) norm;
+    decltype(&spin_layernorm_workspace_bytes) norm_bytes;
+    decltype(&spin_layernorm_grad) norm_grad;
+    decltype(&spin_layernorm_grad_workspace_bytes) norm_grad_bytes;
 };
 template <> struct ByWord<uint32_t> {
     static constexpr at::ScalarType type = at::kInt;
@@ -49,6 +58,15 @@ template <> struct ByWord<uint32_t> {
     decltype(&spin32_cache_values_workspace_bytes) values_bytes;
     decltype(&spin32_relbias_trunc) bias;
     decltype(&spin32_relbias_grad) grad;
+    decltype(&spin32_linattn_scores) linattn_scores;
+    decltype(&spin32_linattn_states) linattn_states;
+    decltype(&spin32_linattn_states_workspace_bytes) linattn_states_bytes;
+    decltype(&spin32_linattn_outputs) linattn_outputs;
+    decltype(&spin32_linattn_step) linattn_step;
+    decltype(&spin32_layernorm) norm;
+    decltype(&spin32_layernorm_workspace_bytes) norm_bytes;
+    decltype(&spin32_layernorm_grad) norm_grad;
+    decltype(&spin32_layernorm_grad_workspace_bytes) norm_grad_bytes;
 };
 struct Library {
     decltype(&spin_share) share, bshare;
@@ -611,6 +629,254 @@ template <class T> PyObject *relbias_grad(PyObject *const *a)      // dS, bucket
     const int causal = a[4] == Py_True;
     return run(*out.t, [&](spin_stream q) { return by_word<T>().grad(p.d[0], p.d[1], p.d[2], p.d[3], p.d[4], p.first, causal, p.lengths, dS, &bias, to, q); });
 }
+// ---- linear attention with a decay, layer norm: (word bits, the arguments of the calls in spin.py) ------------------------------
+// Operands of one call: shapes and that all are on the current device, whose stream the kernels run on.
+template <class T> struct Operands {
+    const int device = c10::hip::current_device();
+    const at::Tensor *ring(PyObject *o, Shape shape) const
+    {
+        const at::Tensor *t = word_tensor<T>(o, shape);
+        return t && t->get_device() == device ? t : nullptr;
+    }
+    bool word(PyObject *o, Shape shape, const T *&p) const
+    {
+        const at::Tensor *t = ring(o, shape);
+        if (t) p = data<T>(t);
+        return t != nullptr;
+    }
+    bool masked(PyObject *o, Shape shape, spin_masked &m) const
+    {
+        const T *x, *a;
+        if (!sequence(o, 2) || !word(PySequence_Fast_GET_ITEM(o, 0), shape, x) || !word(PySequence_Fast_GET_ITEM(o, 1), shape, a)) return false;
+        m = spin_masked{x, a};
+        return true;
+    }
+    bool tuple(PyObject *o, Shape shape, spin_tuple &m) const
+    {
+        const T *r[3];
+        if (!sequence(o, 3)) return false;
+        for (int k = 0; k < 3; ++k)
+            if (!word(PySequence_Fast_GET_ITEM(o, k), shape, r[k])) return false;
+        m = spin_tuple{r[0], r[1], r[2]};
+        return true;
+    }
+    // heads, their decay, and the lengths (or which sequences are active)
+    bool heads(Shape x, int64_t tokens, int64_t chunk, PyObject *f, PyObject *decay, PyObject *g, PyObject *lengths, spin_linattn &s) const
+    {
+        const int most = ByWord<T>::bits - 3;
+        if (!parties(x[0]) || !fits({x[1], x[2], tokens, chunk}) || !integer(f, 1, most, s.f) || !integer(g, 0, most, s.g)) return false;
+        s.n = (int)x[0], s.batch = (int)x[1], s.heads = (int)x[2], s.tokens = (int)tokens, s.chunk = (int)chunk;
+        s.decay = nullptr;
+        if (decay != Py_None) {
+            const int64_t shape[2] = {x[2], chunk + 1};
+            const T *w;
+            if (!word(decay, Shape(shape, 2), w)) return false;
+            s.decay = w;
+        }
+        if (!list_of(lengths, x.slice(1, 1), s.lengths)) return false;
+        return !s.lengths || THPVariable_Unpack(lengths).get_device() == device;
+    }
+    // `out` (which may be longer) or a fresh tensor
+    bool result(PyObject *out, Shape shape, const at::Tensor &like, Result<T> &r) const { return r.take(out, shape, like) && r.t->get_device() == device; }
+};
+template <class T> inline const at::Tensor *first_of(PyObject *pair, int64_t dims)
+{
+    const at::Tensor *t = sequence(pair, 2) ? word_tensor<T>(PySequence_Fast_GET_ITEM(pair, 0)) : nullptr;
+    return t && t->dim() == dims ? t : nullptr;
+}
+inline PyObject *item(PyObject *o, Py_ssize_t k) { return o == Py_None ? Py_None : PySequence_Fast_GET_ITEM(o, k); }
+// Several results, or the status.
+template <class F> inline PyObject *run_all(std::initializer_list<const at::Tensor *> results, F &&call)
+{
+    THPObjectPtr all(PyTuple_New((Py_ssize_t)results.size()));
+    if (!all) return PyErr_Clear(), none();
+    Py_ssize_t k = 0;
+    for (const at::Tensor *t : results) {
+        PyObject *o = t ? THPVariable_Wrap(*t) : none();
+        if (!o) return PyErr_Clear(), none();
+        PyTuple_SET_ITEM(all.get(), k++, o);
+    }
+    const spin_status st = unlocked(call);
+    return st == SPIN_OK ? all.release() : PyLong_FromLong(st);
+}
+struct Workspace {
+    at::Tensor fresh;
+    const at::Tensor *t = nullptr;
+    bool take(PyObject *o, size_t need, const at::Tensor &like)
+    {
+        if (o != Py_None) return (t = workspace_tensor(o)) && t->get_device() == like.get_device();
+        if (need == 0 || need > unasked_bytes) return false;
+        fresh = at::empty({(int64_t)need}, like.options().dtype(at::kByte));
+        t = &fresh;
+        return true;
+    }
+    void *space() const { return t->mutable_data_ptr(); }
+    size_t bytes() const { return (size_t)t->numel() * t->element_size(); }
+};
+
+template <class T> PyObject *linattn_scores(PyObject *const *a)    // x, y, C, tuple, f, decay, g, lengths, out
+{
+    const Operands<T> ops;
+    const at::Tensor *x = first_of<T>(a[0], 5), *C = word_tensor<T>(a[2]);
+    if (!x || !C || C->dim() != 6 || C->size(5) < 1) return none();
+    const Shape s = x->sizes();
+    const int64_t chunk = C->size(5), pairs[6] = {s[0], s[1], s[2], (s[3] + chunk - 1) / chunk, chunk, chunk};
+    spin_linattn d;
+    spin_masked mx, my;
+    spin_tuple t;
+    const T *c;
+    Result<T> out;
+    if (!ops.heads(s, s[3], chunk, a[4], a[5], a[6], a[7], d) || !fits({s[4]}) || !ops.masked(a[0], s, mx) || !ops.masked(a[1], s, my) ||
+        !ops.word(a[2], Shape(pairs, 6), c) || !ops.tuple(a[3], Shape(pairs, 6), t) || !ops.result(a[8], Shape(pairs, 6), *C, out))
+        return none();
+    T *to = data<T>(out.t);
+    return run(*out.t, [&](spin_stream q) { return by_word<T>().linattn_scores(&d, (int)s[4], &mx, &my, c, &t, to, q); });
+}
+template <class T> PyObject *linattn_states(PyObject *const *a)    // x, y, C, tuple, f, chunk, decay, g, lengths, first, reverse, out, workspace
+{
+    const Operands<T> ops;
+    const at::Tensor *x = first_of<T>(a[0], 5), *y = first_of<T>(a[1], 5), *C = word_tensor<T>(a[2]);
+    int chunk;
+    if (!x || !y || !C || !integer(a[5], 1, 0x7fffff, chunk) || !PyBool_Check(a[10]) || (a[11] != Py_None && !sequence(a[11], 2))) return none();
+    const Shape s = x->sizes();
+    const int64_t rows = s[4], columns = y->size(4), state[5] = {s[0], s[1], s[2], rows, columns};
+    const int64_t every[6] = {s[0], s[1], s[2], (s[3] + chunk - 1) / chunk, rows, columns}, values[5] = {s[0], s[1], s[2], s[3], columns};
+    spin_linattn d;
+    spin_masked mx, my;
+    spin_tuple t;
+    const T *c, *first = nullptr;
+    Result<T> states, last;
+    Workspace ws;
+    if (!ops.heads(s, s[3], chunk, a[4], a[6], a[7], a[8], d) || !fits({rows, columns}) || !ops.masked(a[0], s, mx) || !ops.masked(a[1], Shape(values, 5), my) ||
+        !ops.word(a[2], Shape(every, 6), c) || !ops.tuple(a[3], Shape(every, 6), t) || (a[9] != Py_None && !ops.word(a[9], Shape(state, 5), first)) ||
+        !ops.result(item(a[11], 0), Shape(every, 6), *C, states) || !ops.result(item(a[11], 1), Shape(state, 5), *C, last) ||
+        !ws.take(a[12], by_word<T>().linattn_states_bytes(&d, (int)rows, (int)columns), *C))
+        return none();
+    T *to = data<T>(states.t), *end = data<T>(last.t);
+    const int reverse = a[10] == Py_True;
+    return run_all({states.t, last.t}, [&](spin_stream q) {
+        return by_word<T>().linattn_states(&d, (int)rows, (int)columns, reverse, &mx, &my, c, &t, first, to, end, ws.space(), ws.bytes(), q);
+    });
+}
+template <class T> PyObject *linattn_outputs(PyObject *const *a)   // P, y, x, S, C, tuple, f, decay, g, lengths, reverse, transposed, out
+{
+    const Operands<T> ops;
+    const at::Tensor *P = first_of<T>(a[0], 6), *x = first_of<T>(a[2], 5), *C = word_tensor<T>(a[4]);
+    if (!P || !x || !C || C->dim() != 5 || P->size(5) < 1 || !PyBool_Check(a[10]) || !PyBool_Check(a[11])) return none();
+    const Shape s = x->sizes();
+    const bool reverse = a[10] == Py_True, transposed = a[11] == Py_True;
+    const int64_t rows = s[4], columns = C->size(4), chunk = P->size(5), chunks = (s[3] + chunk - 1) / chunk;
+    const int64_t values[5] = {s[0], s[1], s[2], s[3], columns}, pairs[6] = {s[0], s[1], s[2], chunks, chunk, chunk};
+    const int64_t state[6] = {s[0], s[1], s[2], chunks, transposed ? columns : rows, transposed ? rows : columns};
+    spin_linattn d;
+    spin_masked mp, my, mx, ms;
+    spin_tuple t;
+    const T *c;
+    Result<T> out;
+    if (!ops.heads(s, s[3], chunk, a[6], a[7], a[8], a[9], d) || !fits({rows, columns}) || !ops.masked(a[0], Shape(pairs, 6), mp) ||
+        !ops.masked(a[1], Shape(values, 5), my) || !ops.masked(a[2], s, mx) || !ops.masked(a[3], Shape(state, 6), ms) || !ops.word(a[4], Shape(values, 5), c) ||
+        !ops.tuple(a[5], Shape(values, 5), t) || !ops.result(a[12], Shape(values, 5), *C, out))
+        return none();
+    T *to = data<T>(out.t);
+    return run(*out.t, [&](spin_stream q) {
+        return by_word<T>().linattn_outputs(&d, (int)rows, (int)columns, reverse, transposed, &mp, &my, &mx, &ms, c, &t, to, q);
+    });
+}
+template <class T> PyObject *linattn_step(PyObject *const *a)      // S, q, k, v, mask, C, tuples, f, decay, g, active, out
+{
+    const Operands<T> ops;
+    const at::Tensor *S = word_tensor<T>(a[0]);
+    if (!S || S->dim() != 5 || !sequence(a[5], 2) || !sequence(a[6], 2) || (a[11] != Py_None && !sequence(a[11], 2))) return none();
+    const Shape s = S->sizes();
+    const int64_t keys[4] = {s[0], s[1], s[2], s[3]}, values[4] = {s[0], s[1], s[2], s[4]};
+    spin_linattn d;
+    spin_masked q, k, v;
+    spin_tuple tS, tO;
+    const T *state, *mask, *CS, *CO;
+    Result<T> result, after;
+    if (!ops.heads(s, 1, 1, a[7], a[8], a[9], a[10], d) || !fits({s[3], s[4]}) || !ops.word(a[0], s, state) || !ops.masked(a[1], Shape(keys, 4), q) ||
+        !ops.masked(a[2], Shape(keys, 4), k) || !ops.masked(a[3], Shape(values, 4), v) || !ops.word(a[4], s, mask) ||
+        !ops.word(PySequence_Fast_GET_ITEM(a[5], 0), s, CS) || !ops.word(PySequence_Fast_GET_ITEM(a[5], 1), Shape(values, 4), CO) ||
+        !ops.tuple(PySequence_Fast_GET_ITEM(a[6], 0), s, tS) || !ops.tuple(PySequence_Fast_GET_ITEM(a[6], 1), Shape(values, 4), tO) ||
+        !ops.result(item(a[11], 0), Shape(values, 4), *S, result) || !ops.result(item(a[11], 1), s, *S, after))
+        return none();
+    T *to = data<T>(result.t), *next = data<T>(after.t);
+    return run_all({result.t, after.t}, [&](spin_stream stream) {
+        return by_word<T>().linattn_step(&d, (int)s[3], (int)s[4], state, &q, &k, &v, mask, CS, &tS, CO, &tO, next, to, stream);
+    });
+}
+// [n, rows, dim], f, shift
+template <class T> inline bool norm_of(const at::Tensor *x, PyObject *f, PyObject *shift, spin_norm &s)
+{
+    const int most = ByWord<T>::bits - 3;
+    if (!x || x->dim() != 3 || !parties(x->size(0)) || !fits({x->size(1), x->size(2)}) || !integer(f, 1, most - 1, s.f) || !integer(shift, 1, most, s.shift)) return false;
+    s.n = (int)x->size(0), s.rows = (int)x->size(1), s.dim = (int)x->size(2);
+    return true;
+}
+template <class T> PyObject *layernorm(PyObject *const *a)         // x, gamma, beta, masks, C, tuples, row_words, f, shift, line, eps, out, workspace
+{
+    const Operands<T> ops;
+    const at::Tensor *x = word_tensor<T>(a[0]), *w = word_tensor<T>(a[6]);
+    spin_norm d;
+    uint64_t offset, slope, eps;
+    if (!norm_of<T>(x, a[7], a[8], d) || !w || w->dim() != 3 || !fits({w->size(1)}) || w->size(1) % 15 != 0 || !sequence(a[3], 2) || !sequence(a[4], 2) || !sequence(a[5], 2) ||
+        !sequence(a[9], 2) || !word(PySequence_Fast_GET_ITEM(a[9], 0), offset) || !word(PySequence_Fast_GET_ITEM(a[9], 1), slope) || !word(a[10], eps) ||
+        (a[11] != Py_None && !sequence(a[11], 3)))
+        return none();
+    const Shape s = x->sizes();
+    const int64_t columns[2] = {s[0], s[2]}, words[3] = {s[0], w->size(1), s[1]}, rows[2] = {s[0], s[1]};
+    spin_masked gamma;
+    spin_tuple t[2];
+    const T *value, *beta, *mask[2], *C[2], *row_words;
+    Result<T> out, xhat, rstd;
+    Workspace ws;
+    // xhat and rstd may be left out
+    const bool keeps_xhat = a[11] == Py_None || PySequence_Fast_GET_ITEM(a[11], 1) != Py_None, keeps_rstd = a[11] == Py_None || PySequence_Fast_GET_ITEM(a[11], 2) != Py_None;
+    if (!ops.word(a[0], s, value) || !ops.masked(a[1], Shape(columns, 2), gamma) || !ops.word(a[2], Shape(columns, 2), beta) || !ops.word(a[6], Shape(words, 3), row_words))
+        return none();
+    for (int k = 0; k < 2; ++k)
+        if (!ops.word(PySequence_Fast_GET_ITEM(a[3], k), s, mask[k]) || !ops.word(PySequence_Fast_GET_ITEM(a[4], k), s, C[k]) ||
+            !ops.tuple(PySequence_Fast_GET_ITEM(a[5], k), s, t[k]))
+            return none();
+    if (!ops.result(item(a[11], 0), s, *x, out) || (keeps_xhat && !ops.result(item(a[11], 1), s, *x, xhat)) ||
+        (keeps_rstd && !ops.result(item(a[11], 2), Shape(rows, 2), *x, rstd)) || !ws.take(a[12], by_word<T>().norm_bytes(&d), *x))
+        return none();
+    T *to = data<T>(out.t), *to_xhat = keeps_xhat ? data<T>(xhat.t) : nullptr, *to_rstd = keeps_rstd ? data<T>(rstd.t) : nullptr;
+    const int iterations = (int)(w->size(1) / 15) - 1;
+    return run_all({out.t, xhat.t, rstd.t}, [&](spin_stream q) {
+        return by_word<T>().norm(&d, iterations, (T)offset, (T)slope, (T)eps, value, &gamma, beta, mask[0], mask[1], C[0], &t[0], C[1], &t[1], row_words, to, to_xhat, to_rstd,
+                                 ws.space(), ws.bytes(), q);
+    });
+}
+template <class T> PyObject *layernorm_grad(PyObject *const *a)    // dy, xhat, rstd, gamma, masks, C, tuples, row_words, column_words, f, shift, out, workspace
+{
+    const Operands<T> ops;
+    const at::Tensor *dy = word_tensor<T>(a[0]);
+    spin_norm d;
+    if (!norm_of<T>(dy, a[9], a[10], d) || !sequence(a[4], 3) || !sequence(a[5], 2) || !sequence(a[6], 2) || (a[11] != Py_None && !sequence(a[11], 3))) return none();
+    const Shape s = dy->sizes();
+    const int64_t columns[2] = {s[0], s[2]}, row[2] = {s[0], s[1]}, words[3] = {s[0], 22, s[1]}, four[3] = {s[0], 4, s[2]};
+    spin_masked gamma;
+    spin_tuple t[2];
+    const T *value, *xhat, *rstd, *mask[3], *C[2], *row_words, *column_words;
+    Result<T> dx, dgamma, dbeta;
+    Workspace ws;
+    if (!ops.word(a[0], s, value) || !ops.word(a[1], s, xhat) || !ops.word(a[2], Shape(row, 2), rstd) || !ops.masked(a[3], Shape(columns, 2), gamma) ||
+        !ops.word(a[7], Shape(words, 3), row_words) || !ops.word(a[8], Shape(four, 3), column_words))
+        return none();
+    for (int k = 0; k < 3; ++k)
+        if (!ops.word(PySequence_Fast_GET_ITEM(a[4], k), s, mask[k])) return none();
+    for (int k = 0; k < 2; ++k)
+        if (!ops.word(PySequence_Fast_GET_ITEM(a[5], k), s, C[k]) || !ops.tuple(PySequence_Fast_GET_ITEM(a[6], k), s, t[k])) return none();
+    if (!ops.result(item(a[11], 0), s, *dy, dx) || !ops.result(item(a[11], 1), Shape(columns, 2), *dy, dgamma) ||
+        !ops.result(item(a[11], 2), Shape(columns, 2), *dy, dbeta) || !ws.take(a[12], by_word<T>().norm_grad_bytes(&d), *dy))
+        return none();
+    const spin_masked m_dy{value, mask[0]}, m_xhat{xhat, mask[1]};
+    T *to = data<T>(dx.t), *to_gamma = data<T>(dgamma.t), *to_beta = data<T>(dbeta.t);
+    return run_all({dx.t, dgamma.t, dbeta.t}, [&](spin_stream q) {
+        return by_word<T>().norm_grad(&d, &m_dy, &m_xhat, rstd, &gamma, mask[2], C[0], &t[0], C[1], &t[1], row_words, column_words, to, to_gamma, to_beta, ws.space(), ws.bytes(), q);
+    });
+}
 // The first argument says which words; `count` follow.
 inline PyObject *either(PyObject *const *a, Py_ssize_t got, Py_ssize_t count, PyObject *(*wide)(PyObject *const *), PyObject *(*narrow)(PyObject *const *))
 {
@@ -657,6 +923,12 @@ PyMethodDef methods[] = {{"bind", (PyCFunction)(void *)bind, METH_FASTCALL, null
                          FAST("cache_values", either(a, count, 11, cache_values<uint64_t>, cache_values<uint32_t>)),
                          FAST("relbias_trunc", either(a, count, 10, relbias_trunc<uint64_t>, relbias_trunc<uint32_t>)),
                          FAST("relbias_grad", either(a, count, 7, relbias_grad<uint64_t>, relbias_grad<uint32_t>)),
+                         FAST("linattn_scores", either(a, count, 9, linattn_scores<uint64_t>, linattn_scores<uint32_t>)),
+                         FAST("linattn_states", either(a, count, 13, linattn_states<uint64_t>, linattn_states<uint32_t>)),
+                         FAST("linattn_outputs", either(a, count, 13, linattn_outputs<uint64_t>, linattn_outputs<uint32_t>)),
+                         FAST("linattn_step", either(a, count, 12, linattn_step<uint64_t>, linattn_step<uint32_t>)),
+                         FAST("layernorm", either(a, count, 13, layernorm<uint64_t>, layernorm<uint32_t>)),
+                         FAST("layernorm_grad", either(a, count, 13, layernorm_grad<uint64_t>, layernorm_grad<uint32_t>)),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

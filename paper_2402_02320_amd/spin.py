@@ -142,7 +142,8 @@ def _load_binding(L):
                "completed_square_trunc")
     entries = ["spin_" + e for e in entries] + [pre + e for pre in ("spin_", "spin32_") for e in
                                                 ("cache_append", "cache_copy", "cache_compact", "cache_scores", "cache_values", "cache_values_workspace_bytes",
-                                                 "relbias_trunc", "relbias_grad")]
+                                                 "relbias_trunc", "relbias_grad", "linattn_scores", "linattn_states", "linattn_states_workspace_bytes", "linattn_outputs",
+                                                 "linattn_step", "layernorm", "layernorm_workspace_bytes", "layernorm_grad", "layernorm_grad_workspace_bytes")]
     binding.bind(tuple(ctypes.cast(getattr(L, e), ctypes.c_void_p).value for e in entries), _UNASKED_BYTES)
     _fast = binding
 
@@ -977,6 +978,10 @@ class _Word:
         """Scores of linear attention within chunks, T(C[i, j] + w[i - j] x_i . y_j, f + g) for tokens j <= i of a chunk that are there, else zero.
         x, y: (shares, masks), [n, batch, heads, tokens, dim]; C, the truncation tuple and the result: [n, batch, heads, chunks, chunk, chunk], which says how long a chunk
         is (32, 64 or 128).  decay: public words w [heads, chunk + 1], round(lambda^j 2^g), or None; lengths: tokens of every sequence, if not all."""
+        if _fast is not None:
+            done = _fast.linattn_scores(self.bits, x, y, C, tuple_, f, decay, g, lengths, out)
+            if done is not None:
+                return _done(done)
         _shapes(x[0].dim() == 5 and C.dim() == 6)
         n, batch, heads, tokens, dim, chunk = _ints(*x[0].shape, C.shape[5])
         _shapes(chunk > 0)
@@ -996,6 +1001,10 @@ class _Word:
         """States of linear attention: (states, last), the state before every chunk and behind the last, from `first` (None: zeros) on.  A chunk of L > 0 tokens makes
         S <- T(C + 2^f w[L] S + sum_j w[L - 1 - j] x_j (x) y_j, f + g).  reverse: chunks from the last, weights w[j + 1], as the gradient goes.
         x, y: (shares, masks), [n, batch, heads, tokens, rows or columns]; C, the tuple and states: [n, batch, heads, chunks, rows, columns]; out: (states, last)."""
+        if _fast is not None:
+            done = _fast.linattn_states(self.bits, x, y, C, tuple_, f, chunk, decay, g, lengths, first, reverse, out, workspace)
+            if done is not None:
+                return _done(done)
         _shapes(x[0].dim() == 5 and y[0].dim() == 5)
         n, batch, heads, tokens, rows, columns, chunk = _ints(*x[0].shape, y[0].shape[4], chunk)
         _shapes(chunk > 0)
@@ -1018,6 +1027,10 @@ class _Word:
         """T(C_i + 2^g sum_{j <= i} P_ij y_j + w[i + 1] x_i . S, f + g) for the tokens i that are there, else zero; reverse: P_ji, i <= j, and w[L - 1 - i].
         All factors are (shares, masks): P [n, batch, heads, chunks, chunk, chunk], y [n, batch, heads, tokens, columns], x [.., tokens, rows], S [.., chunks, rows, columns],
         or [.., chunks, columns, rows] if transposed.  C, the tuple and the result: as y."""
+        if _fast is not None:
+            done = _fast.linattn_outputs(self.bits, P, y, x, S, C, tuple_, f, decay, g, lengths, reverse, transposed, out)
+            if done is not None:
+                return _done(done)
         _shapes(P[0].dim() == 6 and x[0].dim() == 5 and C.dim() == 5)
         n, batch, heads, tokens, rows, columns, chunk = _ints(*x[0].shape, C.shape[4], P[0].shape[5])
         _shapes(chunk > 0)
@@ -1035,6 +1048,10 @@ class _Word:
         """One token of every sequence (with active[b] > 0, if given): (result, S'), S' = T(C[0] + 2^f w[1] S + w[0] k (x) v, f + g), result = T(C[1] + q . S', f).
         The others keep their state and get zeros.  S, mask (of S'), C[0] and tuples[0]: [n, batch, heads, rows, columns]; q, k: (shares, masks), [n, batch, heads, rows]; v
         likewise of columns, as C[1], tuples[1] and the result; decay: [heads, 2].  out: (result, S'), and S' may be S."""
+        if _fast is not None:
+            done = _fast.linattn_step(self.bits, S, q, k, v, mask, C, tuples, f, decay, g, active, out)
+            if done is not None:
+                return _done(done)
         _shapes(S.dim() == 5)
         n, batch, heads, rows, columns = _ints(*S.shape)
         state, value = tuple(S.shape), (n, batch, heads, columns)
@@ -1068,6 +1085,10 @@ class _Word:
         """Layer norm of rows x [n, rows, dim]: (result, xhat, rstd).  gamma: (shares, masks), [n, dim], as beta; masks, C, tuples: two each, of the centred rows and of
         xhat, all as x; row_words: [n, 15 (iterations + 1), rows], in the order listed at spin_layernorm.  Means are sums times round(2^shift / dim), truncated by shift;
         1 / sqrt(variance + eps) is Newton's from the public line (offset, slope), offset - slope * variance; eps, offset, slope: words at f bits."""
+        if _fast is not None:
+            done = _fast.layernorm(self.bits, x, gamma, beta, masks, C, tuples, row_words, f, shift, line, eps, out, workspace)
+            if done is not None:
+                return _done(done)
         s = self._norm(x, f, shift)
         n, rows, dim = shape = tuple(x.shape)
         _shapes(row_words.dim() == 3 and row_words.shape[1] % 15 == 0 and row_words.shape[1] > 0)
@@ -1085,6 +1106,10 @@ class _Word:
     def layernorm_grad(self, dy, xhat, rstd, gamma, masks, C, tuples, row_words, column_words, f, shift, out=None, workspace=None):
         """Gradients (of x, gamma, beta) from dy, that of the result of layernorm, and its xhat and rstd.  masks: of dy, xhat and dy * gamma; C, tuples: two each, of
         dy * gamma and of the gradient of x, all as dy [n, rows, dim]; row_words: [n, 22, rows], column_words: [n, 4, dim], as listed at spin_layernorm_grad."""
+        if _fast is not None:
+            done = _fast.layernorm_grad(self.bits, dy, xhat, rstd, gamma, masks, C, tuples, row_words, column_words, f, shift, out, workspace)
+            if done is not None:
+                return _done(done)
         s = self._norm(dy, f, shift)
         n, rows, dim = shape = tuple(dy.shape)
         dx, dgamma, dbeta = (torch.empty_like(dy), dy.new_empty((n, dim)), dy.new_empty((n, dim))) if out is None else out
