@@ -21,7 +21,7 @@ template <int NP, class T> __device__ inline T rstd_of(const NormArgs<T> &a, con
 }
 
 template <int NP, class T, int WAVES, int EACH>
-__global__ __launch_bounds__(kNormBlock<WAVES>, WAVES > 4 ? 4 : 1) void norm_kernel(NormArgs<T> a)
+__global__ __launch_bounds__(kNormBlock<WAVES>, WAVES > 4 ? 4 : 1) void norm_kernel(NormArgs<T> a, bool streamed)
 {
     constexpr int ROWS = kRowsAtOnce<WAVES>, THREADS = 64 * WAVES;
     constexpr bool KEEP = NP * EACH * sizeof(T) <= 128;    // the masks stay in registers
@@ -97,6 +97,7 @@ __global__ __launch_bounds__(kNormBlock<WAVES>, WAVES > 4 ? 4 : 1) void norm_ker
         u32 d = (u32)min(j * THREADS + t, a.dim - 1);
         const bool there = j * THREADS + t < a.dim;
         auto word = [&](const T *array, int i) __attribute__((always_inline)) { return (array + (i * party + first))[d]; };
+        auto dealt = [&](const T *array, int i) __attribute__((always_inline)) { return once(array + (i * party + first) + d); };
         auto column = [&](const T *array, int i) __attribute__((always_inline)) { return (array + (size_t)i * a.dim)[d]; };
         const T e = open[j];
         T top[NP], msb[NP], xhat[NP], g = 0, e2 = 0;
@@ -104,9 +105,9 @@ __global__ __launch_bounds__(kNormBlock<WAVES>, WAVES > 4 ? 4 : 1) void norm_ker
         if (!KEEP) make_new(d);
 #pragma unroll
         for (int i = 0; i < NP; ++i) {
-            c.add(word(a.C1, i) + word(a.t1.r, i));
+            c.add(dealt(a.C1, i) + dealt(a.t1.r, i));
             c.add(e * shared[slot][1 + i] + (KEEP ? mask[j][KEEP ? i : 0] : word(a.mask_x, i)) * fr);
-            top[i] = word(a.t1.r_top, i), msb[i] = word(a.t1.r_msb, i);
+            top[i] = dealt(a.t1.r_top, i), msb[i] = dealt(a.t1.r_msb, i);
         }
         // Where a thread has registers for them all its words are asked for at once; otherwise the second truncation's behind the first's.
         auto first_part = [&]() __attribute__((always_inline)) {
@@ -120,15 +121,15 @@ __global__ __launch_bounds__(kNormBlock<WAVES>, WAVES > 4 ? 4 : 1) void norm_ker
             first_part();
             if (a.xhat && there)
 #pragma unroll
-                for (int i = 0; i < NP; ++i) (a.xhat + (i * party + first))[d] = xhat[i];
+                for (int i = 0; i < NP; ++i) put(streamed, a.xhat + (i * party + first) + d, xhat[i]);
             make_new(d);
         }
         T top2[NP], msb2[NP];
 #pragma unroll
         for (int i = 0; i < NP; ++i) {
             g += column(a.gamma.x, i) - column(a.gamma.a, i);
-            c2.add(word(a.C2, i) + word(a.t2.r, i));
-            top2[i] = word(a.t2.r_top, i), msb2[i] = word(a.t2.r_msb, i);
+            c2.add(dealt(a.C2, i) + dealt(a.t2.r, i));
+            top2[i] = dealt(a.t2.r_top, i), msb2[i] = dealt(a.t2.r_msb, i);
         }
         if (KEEP) first_part();
 #pragma unroll
@@ -136,8 +137,8 @@ __global__ __launch_bounds__(kNormBlock<WAVES>, WAVES > 4 ? 4 : 1) void norm_ker
         if (!there) continue;
 #pragma unroll
         for (int i = 0; i < NP; ++i) {
-            if (KEEP && a.xhat) (a.xhat + (i * party + first))[d] = xhat[i];
-            (a.out + (i * party + first))[d] = c2.truncated(i, top2[i], msb2[i]) + column(a.beta, i);
+            if (KEEP && a.xhat) put(streamed, a.xhat + (i * party + first) + d, xhat[i]);
+            put(streamed, a.out + (i * party + first) + d, c2.truncated(i, top2[i], msb2[i]) + column(a.beta, i));
         }
         __builtin_amdgcn_sched_barrier(0);                 // a column's words at a time
     }
@@ -150,6 +151,7 @@ size_t layernorm_workspace(int, int, int, int) { return 256; }
 template <class T> spin_status launch_layernorm(const NormArgs<T> &a, hipStream_t s)
 {
     KernelTimer timer(SPIN_KERNEL_LAYERNORM, s);
+    const bool streamed = (size_t)a.n * a.rows * a.dim * sizeof(T) >= kStreamingBytes;
     spin_status st = SPIN_OK;
     for_party_count(a.n, [&](auto np) {
         for_dim(a.dim, [&](auto waves, auto each) {
@@ -158,7 +160,7 @@ template <class T> spin_status launch_layernorm(const NormArgs<T> &a, hipStream_
             constexpr int row_bytes = kNormWords * NP * (int)sizeof(T) * ROWS;
             static OncePerDevice lds_flags;
             st = allow_dynamic_lds((const void *)kernel, row_bytes * (SPIN_MAX_NORM_ITERATIONS + 1), lds_flags);
-            if (st == SPIN_OK) kernel<<<(a.rows + ROWS - 1) / ROWS, kNormBlock<WAVES>, row_bytes * (a.iterations + 1), s>>>(a);
+            if (st == SPIN_OK) kernel<<<(a.rows + ROWS - 1) / ROWS, kNormBlock<WAVES>, row_bytes * (a.iterations + 1), s>>>(a, streamed);
         });
     });
     return st != SPIN_OK ? st : check_launch("spin_layernorm");

@@ -9,14 +9,14 @@ namespace {
 // Where registers for those sums are not left (more parties, or words a thread: LEAN) columns_kernel makes them from memory, and no party's words are kept from one use to the next.
 template <int NP, class T, int WAVES, int EACH> constexpr bool kLean = EACH > 4 || NP * sizeof(T) * EACH > (WAVES > 4 ? 96 : 160);
 template <int NP, class T, int WAVES, int EACH>
-__global__ __launch_bounds__(kNormBlock<WAVES>, WAVES > 4 ? 4 : 1) void norm_grad_kernel(NormGradArgs<T> a, int run, T *sums)
+__global__ __launch_bounds__(kNormBlock<WAVES>, WAVES > 4 ? 4 : 1) void norm_grad_kernel(NormGradArgs<T> a, int run, T *sums, bool streamed)
 {
     constexpr int ROWS = kRowsAtOnce<WAVES>, THREADS = 64 * WAVES;
     constexpr bool LEAN = kLean<NP, T, WAVES, EACH>, KEEP = !LEAN && 2 * NP * EACH * sizeof(T) <= (WAVES > 4 ? 64 : 128);
     __shared__ T partial[ROWS][2][WAVES], shared[ROWS][3 * NP + 2], words_of[ROWS][(kNormGradWords + 1) * NP];
     const int slot = WAVES == 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x / 64) : 0, wave = WAVES == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     const int t = threadIdx.x % THREADS;
-    const long group = xcd_contiguous_id(blockIdx.x, gridDim.x) * ROWS + slot;
+    const long group = (long)blockIdx.x * ROWS + slot;
     const long row0 = group * run, row1 = min(row0 + run, (long)a.rows);
     if (row0 >= row1) return;                              // of a whole wave or workgroup
     const size_t party = (size_t)a.rows * a.dim;
@@ -36,6 +36,7 @@ __global__ __launch_bounds__(kNormBlock<WAVES>, WAVES > 4 ? 4 : 1) void norm_gra
             make_new(d);
             const bool there = j * THREADS + t < a.dim;
             auto word = [&](const T *array, int i) __attribute__((always_inline)) { return (array + (i * party + first))[d]; };
+            auto dealt = [&](const T *array, int i) __attribute__((always_inline)) { return once(array + (i * party + first) + d); };
             auto column = [&](const T *array, int i) __attribute__((always_inline)) { return (array + (size_t)i * a.dim)[d]; };
             T fg = 0, e1 = 0, e2 = 0, e3 = 0, z = 0;
             Opened<T> c{a.f};
@@ -49,13 +50,13 @@ __global__ __launch_bounds__(kNormBlock<WAVES>, WAVES > 4 ? 4 : 1) void norm_gra
             if (LEAN) make_new(d);
 #pragma unroll
             for (int i = 0; i < NP; ++i) {
-                c.add(word(a.C1, i) + word(a.t1.r, i));
+                c.add(dealt(a.C1, i) + dealt(a.t1.r, i));
                 c.add(e1 * (column(a.gamma.a, i) + (i == 0 ? fg : 0)) + word(a.dy.a, i) * fg);
                 if (!LEAN) gamma_sum[LEAN ? 0 : j] += e1 * (word(a.xhat.a, i) + (i == 0 ? e2 : 0)) + word(a.dy.a, i) * e2;
             }
 #pragma unroll
             for (int i = 0; i < NP; ++i) {
-                const T g = c.truncated(i, word(a.t1.r_top, i), word(a.t1.r_msb, i));
+                const T g = c.truncated(i, dealt(a.t1.r_top, i), dealt(a.t1.r_msb, i));
                 e3 += g - word(a.mask_g, i);
                 s[0] += there ? g : 0;
             }
@@ -112,19 +113,20 @@ __global__ __launch_bounds__(kNormBlock<WAVES>, WAVES > 4 ? 4 : 1) void norm_gra
             u32 d = (u32)min(j * THREADS + t, a.dim - 1);
             make_new(d);
             auto word = [&](const T *array, int i) __attribute__((always_inline)) { return (array + (i * party + first))[d]; };
+            auto dealt = [&](const T *array, int i) __attribute__((always_inline)) { return once(array + (i * party + first) + d); };
             const T e3 = open_g[j], e2 = open_x[j];
             T top[NP], msb[NP];
             Opened<T> c{a.f};
 #pragma unroll
             for (int i = 0; i < NP; ++i) {
-                c.add(word(a.C2, i) + word(a.t2.r, i));
+                c.add(dealt(a.C2, i) + dealt(a.t2.r, i));
                 c.add(e3 * shared[slot][2 + i] + (KEEP ? mask_g[j][KEEP ? i : 0] : word(a.mask_g, i)) * fr);
                 c.add(0 - (e2 * shared[slot][2 + NP + i] + (KEEP ? mask_x[j][KEEP ? i : 0] : word(a.xhat.a, i)) * ek));
-                top[i] = word(a.t2.r_top, i), msb[i] = word(a.t2.r_msb, i);
+                top[i] = dealt(a.t2.r_top, i), msb[i] = dealt(a.t2.r_msb, i);
             }
             if (j * THREADS + t >= a.dim) continue;
 #pragma unroll
-            for (int i = 0; i < NP; ++i) (a.dx + (i * party + first))[d] = c.truncated(i, top[i], msb[i]) - shared[slot][2 + 2 * NP + i];
+            for (int i = 0; i < NP; ++i) put(streamed, a.dx + (i * party + first) + d, c.truncated(i, top[i], msb[i]) - shared[slot][2 + 2 * NP + i]);
             __builtin_amdgcn_sched_barrier(0);
         }
         row_barrier<WAVES>();
@@ -225,12 +227,13 @@ template <class T> spin_status launch_layernorm_grad(const NormGradArgs<T> &a, h
 {
     KernelTimer timer(SPIN_KERNEL_LAYERNORM, s);
     const Runs r = runs_of(a.rows, a.dim);
+    const bool streamed = (size_t)a.n * a.rows * a.dim * sizeof(T) >= kStreamingBytes;
     T *const sums = (T *)a.workspace;
     for_party_count(a.n, [&](auto np) {
         constexpr int NP = decltype(np)::value;
         for_dim(a.dim, [&](auto waves, auto each) {
             constexpr int WAVES = decltype(waves)::value, ROWS = kRowsAtOnce<WAVES>;
-            norm_grad_kernel<NP, T, WAVES, decltype(each)::value><<<(unsigned)((r.groups + ROWS - 1) / ROWS), kNormBlock<WAVES>, 0, s>>>(a, r.run, sums);
+            norm_grad_kernel<NP, T, WAVES, decltype(each)::value><<<(unsigned)((r.groups + ROWS - 1) / ROWS), kNormBlock<WAVES>, 0, s>>>(a, r.run, sums, streamed);
             if constexpr (kLean<NP, T, WAVES, decltype(each)::value>)
                 columns_kernel<NP, T><<<dim3((a.dim + 63) / 64, (unsigned)r.groups), 64 * kColumnRows, 0, s>>>(a, r.run, sums);
         });

@@ -21,14 +21,6 @@ template <int NP, class T> __device__ inline Factor<NP, T> factor(const Masked<T
     }
     return f;
 }
-// The sum over the parties of their parts of a product, each from its own mask.
-template <int NP, class T> __device__ inline T product(const Factor<NP, T> &x, const Factor<NP, T> &y)
-{
-    T z = 0;
-#pragma unroll
-    for (int i = 0; i < NP; ++i) z += x.open * (i == 0 ? y.mask[i] + y.open : y.mask[i]) + x.mask[i] * y.open;
-    return z;
-}
 template <class T> __device__ inline T weight(const T *decay, int head, int chunk, int j) { return decay ? decay[(size_t)head * (chunk + 1) + j] : 1; }
 
 // One element of a result whose parties' products sum to z.
@@ -39,9 +31,9 @@ template <int NP, class T> __device__ inline void finish(T z, const T *C, const 
     T top[NP], msb[NP];
 #pragma unroll
     for (int i = 0; i < NP; ++i) {
-        c.add(C[i * party + at] + t.r[i * party + at]);
-        top[i] = t.r_top[i * party + at];
-        msb[i] = t.r_msb[i * party + at];
+        c.add(once(C + i * party + at) + once(t.r + i * party + at));
+        top[i] = once(t.r_top + i * party + at);
+        msb[i] = once(t.r_msb + i * party + at);
     }
 #pragma unroll
     for (int i = 0; i < NP; ++i) out[i * party + at] = c.truncated(i, top[i], msb[i]);
@@ -385,7 +377,7 @@ template <int NP, class T> __global__ __launch_bounds__(kProductBlock, 2) void s
         const size_t to = at.unit * state + (size_t)(r0 + r) * a.columns + d0 + d;
         T z = ((const T *)lds)[r * kPitch + d];
 #pragma unroll
-        for (int i = 0; i < NP; ++i) z += a.C[i * each + to] + a.t.r[i * each + to];
+        for (int i = 0; i < NP; ++i) z += once(a.C + i * each + to) + once(a.t.r + i * each + to);
         a.opened[to] = z;
     }
 }
@@ -459,54 +451,77 @@ template <int NP, class T> __global__ __launch_bounds__(kBlock) void scan_kernel
     for (int i = 0; i < NP; ++i) a.last[i * one + (size_t)blockIdx.y * state + u] = S[i];
 }
 
-// blockIdx.x: 64 columns, of which a thread has one of every fourth row.
-template <int NP, class T> __global__ __launch_bounds__(kBlock) void step_kernel(StepArgs<T> a)
+// ---- a single token -----------------------------------------------------------------------------------------
+// A workgroup has `wide` columns of one head's state (a power of two), a thread one of them and every (kStepBlock / wide)-th row: all words of a state element are read and
+// written once, 7 a party, and what q . S' takes of them is added in registers, then in LDS.
+constexpr int kStepBlock = 256;
+template <int NP, class T> __global__ __launch_bounds__(kStepBlock) void step_kernel(StepArgs<T> a, int wide, bool streamed)
 {
-    __shared__ T sums[kBlock];
-    const int d = blockIdx.x * 64 + threadIdx.x % 64, part = threadIdx.x / 64, b = blockIdx.y / a.heads, h = blockIdx.y % a.heads;
+    constexpr int kMostRows = 256;
+    __shared__ T keys[kMostRows][NP + 1], queries[kMostRows][NP + 1], sums[kStepBlock];
+    const int lane = threadIdx.x % wide, part = threadIdx.x / wide, parts = kStepBlock / wide, d = blockIdx.x * wide + lane, b = blockIdx.y / a.heads, h = blockIdx.y % a.heads;
     const size_t heads = (size_t)a.batch * a.heads, one = heads * a.rows * a.columns;
     const bool live = !a.active || a.active[b] > 0, mine = d < a.columns;
+    const size_t first = (size_t)blockIdx.y * a.rows * a.columns + min(d, a.columns - 1);
+    if (!live) {                                           // of a whole workgroup
+        if (!mine) return;
+        if (a.S_out != a.S)
+            for (int r = part; r < a.rows; r += parts)
+#pragma unroll
+                for (int i = 0; i < NP; ++i) a.S_out[i * one + first + (size_t)r * a.columns] = a.S[i * one + first + (size_t)r * a.columns];
+        if (part == 0)
+#pragma unroll
+            for (int i = 0; i < NP; ++i) a.out[i * heads * a.columns + (size_t)blockIdx.y * a.columns + d] = 0;
+        return;
+    }
+    for (int k = threadIdx.x; k < 2 * a.rows; k += kStepBlock) {
+        const int r = k % a.rows;
+        const Factor<NP, T> f = factor<NP>(k < a.rows ? a.k : a.q, heads * a.rows, (size_t)blockIdx.y * a.rows + r);
+        T *const to = k < a.rows ? keys[r] : queries[r];
+        to[NP] = f.open;
+#pragma unroll
+        for (int i = 0; i < NP; ++i) to[i] = f.mask[i];
+    }
+    const T w0 = weight(a.decay, h, 1, 0), w1 = weight(a.decay, h, 1, 1) << a.f;
+    const Factor<NP, T> v = factor<NP>(a.v, heads * a.columns, (size_t)blockIdx.y * a.columns + min(d, a.columns - 1));
+    __syncthreads();
     T sum = 0;
-    if (mine) {
-        const T w0 = weight(a.decay, h, 1, 0), w1 = weight(a.decay, h, 1, 1) << a.f;
-        const Factor<NP, T> v = factor<NP>(a.v, heads * a.columns, (size_t)blockIdx.y * a.columns + d);
-        for (int r = part; r < a.rows; r += kBlock / 64) {
-            const size_t at = ((size_t)blockIdx.y * a.rows + r) * a.columns + d;
-            T S[NP];
+    for (int r = mine ? part : a.rows; r < a.rows; r += parts) {
+        const size_t at = first + (size_t)r * a.columns;
+        T S[NP], top[NP], msb[NP], mask[NP], dealt[NP];
+        Opened<T> c{a.f + a.g};
 #pragma unroll
-            for (int i = 0; i < NP; ++i) S[i] = a.S[i * one + at];
-            if (live) {
-                Opened<T> c{a.f + a.g};
-                Factor<NP, T> s;
-                T top[NP], msb[NP];
-                c.add(w0 * product(factor<NP>(a.k, heads * a.rows, (size_t)blockIdx.y * a.rows + r), v));
-#pragma unroll
-                for (int i = 0; i < NP; ++i) {
-                    c.add(w1 * S[i] + a.CS[i * one + at] + a.tS.r[i * one + at]);
-                    top[i] = a.tS.r_top[i * one + at], msb[i] = a.tS.r_msb[i * one + at];
-                    s.mask[i] = a.S_mask[i * one + at];
-                }
-#pragma unroll
-                for (int i = 0; i < NP; ++i) {
-                    S[i] = c.truncated(i, top[i], msb[i]);
-                    s.open += S[i] - s.mask[i];
-                }
-                sum += product(factor<NP>(a.q, heads * a.rows, (size_t)blockIdx.y * a.rows + r), s);
-            }
-#pragma unroll
-            for (int i = 0; i < NP; ++i) a.S_out[i * one + at] = S[i];
+        for (int i = 0; i < NP; ++i) {
+            S[i] = a.S[i * one + at];
+            dealt[i] = once(a.CS + i * one + at) + once(a.tS.r + i * one + at);
+            top[i] = once(a.tS.r_top + i * one + at), msb[i] = once(a.tS.r_msb + i * one + at);
+            mask[i] = once(a.S_mask + i * one + at);
         }
+        T z = 0, open = 0;
+        const T ek = keys[r][NP], eq = queries[r][NP];
+#pragma unroll
+        for (int i = 0; i < NP; ++i) {
+            z += ek * (v.mask[i] + (i == 0 ? v.open : 0)) + keys[r][i] * v.open;
+            c.add(w1 * S[i] + dealt[i]);
+        }
+        c.add(w0 * z);
+#pragma unroll
+        for (int i = 0; i < NP; ++i) {
+            S[i] = c.truncated(i, top[i], msb[i]);
+            open += S[i] - mask[i];
+        }
+#pragma unroll
+        for (int i = 0; i < NP; ++i) {
+            sum += eq * (mask[i] + (i == 0 ? open : 0)) + queries[r][i] * open;
+        }
+#pragma unroll
+        for (int i = 0; i < NP; ++i) put(streamed, a.S_out + i * one + at, S[i]);
     }
     sums[threadIdx.x] = sum;
     __syncthreads();
     if (part || !mine) return;
-    for (int k = 1; k < kBlock / 64; ++k) sum += sums[threadIdx.x + 64 * k];
-    const size_t each = heads * a.columns, at = (size_t)blockIdx.y * a.columns + d;
-    if (live) {
-        finish<NP>(sum, a.CO, a.tO, a.f, each, at, a.out);
-    } else {
-        for (int i = 0; i < NP; ++i) a.out[i * each + at] = 0;
-    }
+    for (int k = 1; k < parts; ++k) sum += sums[threadIdx.x + wide * k];
+    finish<NP>(sum, a.CO, a.tO, a.f, heads * a.columns, (size_t)blockIdx.y * a.columns + d, a.out);
 }
 
 // Launches one of the kernels above on all tiles of all chunks.
@@ -561,8 +576,11 @@ template <class T> spin_status launch_linattn_outputs(const OutputsArgs<T> &a, h
 template <class T> spin_status launch_linattn_step(const StepArgs<T> &a, hipStream_t s)
 {
     KernelTimer timer(SPIN_KERNEL_LINATTN, s);
+    const bool streamed = (size_t)a.n * a.batch * a.heads * a.rows * a.columns * sizeof(T) >= kStreamingBytes;
+    int wide = 64;
+    while (wide > 8 && (long)a.batch * a.heads * ((a.columns + wide - 1) / wide) < 1024) wide /= 2;
     for_party_count(a.n, [&](auto np) {
-        step_kernel<decltype(np)::value, T><<<dim3((a.columns + 63) / 64, a.batch * a.heads), kBlock, 0, s>>>(a);
+        step_kernel<decltype(np)::value, T><<<dim3((a.columns + wide - 1) / wide, a.batch * a.heads), kStepBlock, 0, s>>>(a, wide, streamed);
     });
     return check_launch("spin_linattn_step");
 }

@@ -88,6 +88,17 @@ constexpr int norm_waves(int dim) { return dim <= 256 ? 1 : dim <= 1024 ? 4 : di
 
 namespace {
 
+// A word that is read once, by nobody else: what the dealer gave for one element.
+template <class T> __device__ inline T once(const T *p) { return __builtin_nontemporal_load(p); }
+
+// Results far larger than the caches, all parties', are written past them.
+constexpr size_t kStreamingBytes = (size_t)64 << 20;
+template <class T> __device__ inline void put(bool streamed, T *p, T v)
+{
+    if (streamed) __builtin_nontemporal_store(v, p);
+    else *p = v;
+}
+
 // Tokens of sequence b that are in a chunk.
 __host__ __device__ inline int tokens_in(const ChunkView &c, int b, int chunk)
 {
