@@ -40,20 +40,24 @@ template <int NP, class T> __device__ inline void finish(T z, const T *C, const 
 }
 
 // ---- products within chunks ---------------------------------------------------------------------------------
-// Scores, a chunk's part of the next state and the outputs are products of two secrets within a chunk, [64 rows] x [64 columns] a workgroup: for every party
+// Scores, a chunk's part of the next state and the outputs are products of two secrets within a chunk, [TILE rows] x [TILE columns] a workgroup: for every party
 // E . b_i + a_i . F (+ E . F, party 0), all in one sum, which is all that the parties open.  Words are rewritten as ND balanced digits of eight bits
 // (limb_common.hpp) and multiplied on v_mfma_i32_32x32x32_i8, digit pairs of one diagonal sharing an accumulator (at most 8 pairs x 2 products x 8 parties x
 // 384 k x 2^14 = 2^30 in one).
 //
-// 32 k at a time: the first four waves open and split the left factor, the others the right one, into LDS as MFMA fragments, E and F and up to kGroup
-// parties' masks at a time (a_0 of the right with F added, which folds E . F in); then waves 0 to 3 multiply E . b_i, a 32 x 32 quarter each, and 4 to 7 a_i . F, as F^T . a_i^T so
-// that both keep their one factor's digits in registers.  More parties than kGroup read the others' masks a second time.
-// A factor is stored along its rows or along k; only the left one is cleared where it does not count, and weighed: by row, by k, or by 2^g.
-constexpr int kProductWaves = 8, kProductBlock = 64 * kProductWaves, kTile = 64, kStep = 32, kWords = kTile * kStep / (kProductBlock / 2);
-constexpr int kPitch = kTile + 1;      // of a workgroup's sums in LDS
-template <class T> constexpr int kSlot = 2 * (int)sizeof(T) * kFrag;               // one factor's digits of 64 x 32
-template <int NP, class T> constexpr int kGroup = sizeof(T) == 4 ? NP : NP < 3 ? NP : 3;
-template <int NP, class T> constexpr int product_lds = 2 * (kGroup<NP, T> + 1) * kSlot<T>;
+// 32 k at a time: half of the waves open and split the left factor, half the right one, into LDS as MFMA fragments, E and F and the masks of up to GROUP parties (a_0 of the right
+// with F added, which folds E . F in); then the first half multiplies E . b_i, the others a_i . F, as F^T . a_i^T so that both keep their one factor's digits in registers.
+// Tiles of 64: eight waves, of either product one has a 32 x 32 quarter; more parties than GROUP read the others' masks a second time.  Tiles of 32: four waves, of either product
+// one has every second party; for few chunks, where the larger ones leave CUs idle.
+// A factor is stored along its rows or along k; only the left one is cleared where it does not count, and weighed.
+constexpr int kStep = 32;              // k
+template <int TILE> constexpr int kProductBlock = 8 * TILE;
+template <class T, int TILE> constexpr int kSlot = TILE / 32 * (int)sizeof(T) * kFrag;             // one factor's digits of TILE x 32
+template <int NP, class T, int TILE> constexpr int kGroup = TILE == 32 || NP < 3 ? NP : 3;
+enum Weight { kNone, kByRow, kByK };
+template <int NP, class T, int TILE, Weight W> constexpr int kAhead = TILE == 32 || NP == 1 || NP > kGroup<NP, T, TILE> || (NP == 3 && W != kNone) ? 1 : 2;
+template <int NP, class T, int TILE> constexpr int product_lds = 2 * (kGroup<NP, T, TILE> + 1) * kSlot<T, TILE>;
+template <int NP, class T, int TILE> constexpr int kProductOccupancy = sizeof(T) == 4 && NP > 1 ? 4 : 2;          // waves a SIMD
 
 template <class T> struct Side {       // of a product: rows of the left factor, columns of the right one
     const T *x, *a;                    // of the workgroup's first row and k
@@ -70,20 +74,19 @@ template <class T> __device__ inline Side<T> either(bool second, const Side<T> &
 template <class T> struct Range {      // of k
     int begin, end;                    // whole steps but for the end
     int below, above;                  // row i counts for i + above <= k <= i + below only
-    const T *w;                        // the weight of row 0, or of k = 0; null: all `same`
+    const T *w;                        // the weight of row 0, or of k = 0; null: 1
     int stride;                        // from weight to weight: 1 or -1
-    T same;
+    int shift;                         // and all by 2^shift
 };
 template <class T> __device__ inline Range<T> either(bool second, const Range<T> &a, const Range<T> &b)
 {
     return {second ? b.begin : a.begin, second ? b.end : a.end, second ? b.below : a.below, second ? b.above : a.above, second ? b.w : a.w, second ? b.stride : a.stride,
-            second ? b.same : a.same};
+            second ? b.shift : a.shift};
 }
 template <class T> struct Segment {
     Side<T> left, right;
     Range<T> k;
 };
-enum Weight { kNone, kByRow, kByK };
 
 // The digits of four words: byte e of digit d is digit d of word e.
 template <class T> __device__ inline void digits_of(const T *w, u32 (&d)[sizeof(T)])
@@ -101,159 +104,175 @@ template <class T> __device__ inline void digits_of(const T *w, u32 (&d)[sizeof(
         d[4 * half + 3] = __builtin_amdgcn_perm(t3, t1, 0x07060302u);
     }
 }
-// Where a fragment has 16 k of a row: the second 16 eight rows further, off the first one's banks.
-__device__ inline int place(int row, int half) { return (half * 32 + (row + 8 * half) % 32) * 16; }
+// Where a fragment has half of a row's k: every second row, the others, and either of the second half, all off each other's banks.
+__device__ inline int place(int row, int half) { return (half * 32 + row % 2 * 16 + (row / 2 + row % 2 * 8 + half * 4) % 16) * 16; }
 
-// The sums of a 64 x 64 tile over two ranges of k, in LDS as [64][kPitch] words when it returns (all waves have passed a barrier).
-template <int NP, class T, Weight WEIGH> __device__ inline void product_tile(const Segment<T> &one, const Segment<T> &two, char *lds)
+// The sums of a tile over two ranges of k, in LDS as words when it returns (all waves have passed a barrier): sum_at().
+template <int NP, class T, int TILE, Weight WEIGH> __device__ inline void product_tile(const Segment<T> &one, const Segment<T> &two, char *lds)
 {
-    constexpr int ND = sizeof(T), GROUP = kGroup<NP, T>, kRowsAtOnce = kTile / 2;
-    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
-    const bool right = wave >= kProductWaves / 2;
-    const int quarter = wave % 4;
-    char *const mine = lds + (right ? (GROUP + 1) * kSlot<T> : 0);
+    constexpr int ND = sizeof(T), GROUP = kGroup<NP, T, TILE>, WAVES = TILE / 8, SIDE = 4 * TILE, HALF = TILE / 2, kBlock = ND * kFrag;
+    constexpr int kPitch = TILE + 1;
+    const u32 lane = threadIdx.x % 64;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    const bool right = wave >= WAVES / 2;
+    const u32 u = threadIdx.x % SIDE;  // among the threads of a side
+    char *const rights = lds + (GROUP + 1) * kSlot<T, TILE>, *const mine = right ? rights : lds;
     const Side<T> side0 = either(right, one.left, one.right), side1 = either(right, two.left, two.right);
     auto steps = [](const Range<T> &k) { return k.end > k.begin ? (k.end - k.begin + kStep - 1) / kStep : 0; };
     const int steps0 = steps(one.k), total = steps0 + steps(two.k);
-    // This thread's words of a step: along k four of rows u / 8 and 32 further, along the rows eight k of one row.
-    const int thread = threadIdx.x % (kProductBlock / 2);
-    auto load = [&](T (&w)[kWords], const Side<T> &s, const T *from, int k0) __attribute__((always_inline)) {
-        int u = thread;
-        asm volatile("" : "+v"(u));                        // what follows from the thread's place is made anew, not kept over the products
-        if (s.along) {
-            typedef T vec __attribute__((ext_vector_type(16 / sizeof(T))));
-            constexpr int W = 16 / sizeof(T);
-            const int k = min(k0 + u % 8 * 4, s.ks - 4);
+    // This thread's words of a step: of two rows those at k = 16 (e / 2) + 2 q + e % 2, e < 4; along k the rows u / 8 and HALF further, q = u % 8, along the rows neighbours, q = u /
+    // HALF.  So either way a load has two words, and in a fragment, where k stands in place 4 (k % 16 / 2) + 2 (k / 16) + k % 2, a row's four are neighbours.  No load is
+    // behind a branch: where branches met its words would be copied, and a copy waits for them.
+    typedef T pair __attribute__((ext_vector_type(2)));
+    auto q_of = [&](bool along) __attribute__((always_inline)) { return along ? u % 8 : u / HALF; };
+    auto row_of = [&](bool along, int half) __attribute__((always_inline)) { return along ? u / 8 + half * HALF : u % HALF * 2 + half; };
+    auto k_of = [&](bool along, int e) __attribute__((always_inline)) { return 16 * (e / 2) + e % 2 + 2 * (int)q_of(along); };
+    constexpr int AHEAD = kAhead<NP, T, TILE, WEIGH>;
+    pair x[AHEAD][4], a[AHEAD][4];     // of the parties at hand
+    auto load = [&](const Side<T> &s, int k0, int i, bool masks_only, pair (&value)[4], pair (&mask)[4]) __attribute__((always_inline)) {
+        const T *const px = s.x + i * s.party, *const pa = s.a + i * s.party;
+        const int q = q_of(s.along);
+        const u32 near = s.along ? __umul24(min((int)row_of(true, 0), s.rows - 1), s.pitch) : min((int)row_of(false, 0), s.rows - 2);
+        const u32 far = s.along ? __umul24(min((int)row_of(true, 1), s.rows - 1), s.pitch) : near;
 #pragma unroll
-            for (int half = 0; half < 2; ++half) {
-                const T *p = from + ((u32)min(half * kRowsAtOnce + u / 8, s.rows - 1) * s.pitch + (u32)k);
-#pragma unroll
-                for (int e = 0; e < 4; e += W) {
-                    const vec v = *(const vec *)(p + e);
-#pragma unroll
-                    for (int q = 0; q < W; ++q) w[half * 4 + e + q] = v[q];
-                }
-            }
-        } else {
-            const u32 row = (u32)min(u % 64, s.rows - 1);
-#pragma unroll
-            for (int e = 0; e < kWords; ++e) w[e] = (from + (u32)min(k0 + quarter * kWords + e, s.ks - 1) * s.pitch)[row];
+        for (int v = 0; v < 4; ++v) {
+            const int k = min(k0 + 16 * (s.along ? v % 2 : v / 2) + (s.along ? 0 : v % 2) + 2 * q, s.ks - (s.along ? 2 : 1));
+            const u32 at = (v < 2 ? near : far) + __umul24(k, s.along ? 1 : s.pitch);
+            if (!masks_only) value[v] = *(const pair *)(px + at);
+            mask[v] = *(const pair *)(pa + at);
         }
     };
-    auto stage = [&](const T (&w)[kWords], int slot, bool along) __attribute__((always_inline)) {
-        int u = thread;
-        asm volatile("" : "+v"(u));
-        u32 d[2][ND];
-        digits_of<T>(w, d[0]);
-        digits_of<T>(w + 4, d[1]);
-        char *const to = mine + slot * kSlot<T>;
-        if (along) {
-            char *const at = to + place(u / 8, u % 8 / 4) + u % 4 * 4;
+    auto word_of = [](const pair (&v)[4], bool along, int half, int e) __attribute__((always_inline)) { return along ? v[2 * half + e / 2][e % 2] : v[e][half]; };
+    auto stage = [&](const T (&w)[4], int half, int slot, bool along) __attribute__((always_inline)) {
+        u32 d[ND];
+        digits_of<T>(w, d);
+        const int row = row_of(along, half), q = q_of(along);
+        char *const to = mine + slot * kSlot<T, TILE> + (row / 32 * kBlock + place(row % 32, q / 4) + q % 4 * 4);
 #pragma unroll
-            for (int half = 0; half < 2; ++half)
-#pragma unroll
-                for (int k = 0; k < ND; ++k) *(u32 *)(at + (half * ND + k) * kFrag) = d[half][k];
-        } else {
-            char *const at = to + u % 64 / 32 * (ND * kFrag) + place(u % 32, quarter / 2) + quarter % 2 * 8;
-#pragma unroll
-            for (int k = 0; k < ND; ++k) *(u32x2 *)(at + k * kFrag) = u32x2{d[0][k], d[1][k]};
-        }
+        for (int k = 0; k < ND; ++k) *(u32 *)(to + k * kFrag) = d[k];
     };
     v16i acc[ND];
 #pragma unroll
     for (int d = 0; d < ND; ++d)
 #pragma unroll
         for (int r = 0; r < 16; ++r) acc[d][r] = 0;
-    const int wm = quarter / 2, wn = quarter % 2, lane_at = place(lane % 32, lane / 32);
-    const char *const own = right ? lds + (GROUP + 1) * kSlot<T> + wn * (ND * kFrag) + lane_at : lds + wm * (ND * kFrag) + lane_at;
-    const char *const other = right ? lds + wm * (ND * kFrag) + lane_at : lds + (GROUP + 1) * kSlot<T> + wn * (ND * kFrag) + lane_at;
+    const int wm = TILE == 64 ? wave % 4 / 2 : 0, wn = TILE == 64 ? wave % 2 : 0;
+    const u32 lane_at = place(lane % 32, lane / 32);
+    const char *const own = (right ? rights + wn * kBlock : lds + wm * kBlock) + lane_at, *const other = (right ? lds + wm * kBlock : rights + wn * kBlock) + lane_at;
+    // Tiles of 32: the workgroups of a CU begin with different parties, so that where the parties are odd their SIMDs have the same work.  Four digits of the own factor at a time: all
+    // eight take registers that the next words need.
+    const int begin = TILE == 64 ? 1 : 1 + (wave + blockIdx.x / kXcds) % 2, by = TILE == 64 ? 1 : 2;
     auto multiply = [&](int parties) __attribute__((always_inline)) {
         asm volatile("" : "+s"(parties));                  // a loop for one party, too: unrolled, its products take a second set of sums
-        v4i kept[ND];
 #pragma unroll
-        for (int d = 0; d < ND; ++d) kept[d] = *(const v4i *)(own + d * kFrag);
+        for (int d0 = 0; d0 < ND; d0 += 4) {
+            v4i kept[4];
+#pragma unroll
+            for (int d = 0; d < 4; ++d) kept[d] = *(const v4i *)(own + (d0 + d) * kFrag);
 #pragma unroll 1
-        for (int i = 1; i <= parties; ++i) {
-            const char *const at = other + i * kSlot<T>;
-            v4i ahead = *(const v4i *)at;
+            for (int i = begin; i <= parties; i += by) {
+                const char *const at = other + i * kSlot<T, TILE>;
+                v4i ahead = *(const v4i *)at;
 #pragma unroll
-            for (int p = 0; p < ND; ++p) {                 // one fragment is read ahead: left alone the compiler reads all of them first
-                const v4i b = ahead;
-                if (p + 1 < ND) ahead = *(const v4i *)(at + (p + 1) * kFrag);
-                __builtin_amdgcn_sched_barrier(0);
+                for (int p = 0; p < ND - d0; ++p) {        // one fragment is read ahead: left alone the compiler reads all of them first
+                    const v4i b = ahead;
+                    if (p + 1 < ND - d0) ahead = *(const v4i *)(at + (p + 1) * kFrag);
+                    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                for (int d = 0; d + p < ND; ++d) acc[d + p] = __builtin_amdgcn_mfma_i32_32x32x32_i8(kept[d], b, acc[d + p], 0, 0, 0);
+                    for (int d = 0; d < 4 && d0 + d + p < ND; ++d)
+                        acc[d0 + d + p] = __builtin_amdgcn_mfma_i32_32x32x32_i8(kept[d], b, acc[d0 + d + p], 0, 0, 0);
+                }
             }
         }
     };
-    T x[2][kWords], a[2][kWords];
+    auto word = [&](int r) __attribute__((always_inline)) {
+        T v = 0;
+#pragma unroll
+        for (int d = ND - 1; d >= 0; --d) v = (v << 8) + (T)(std::make_signed_t<T>)acc[d][r];
+        return v;
+    };
     auto load_party = [&](int to, int t, int i) __attribute__((always_inline)) {
         const bool second = t >= steps0;
-        const Side<T> s = either(second, side0, side1);
-        const int k0 = second ? two.k.begin + (t - steps0) * kStep : one.k.begin + t * kStep;
-        load(x[to], s, s.x + i * s.party, k0);
-        load(a[to], s, s.a + i * s.party, k0);
+        load(either(second, side0, side1), second ? two.k.begin + (t - steps0) * kStep : one.k.begin + t * kStep, i, false, x[to], a[to]);
     };
-    T by_row[2] = {1, 1};
-    // The words of the next step's first party are under way during the products; registers for that are left where there is one group.
-    if (NP <= GROUP && total) load_party((NP - 1) % 2, 0, NP - 1);
+    // The words of AHEAD parties are under way, the next step's during the products.
+    auto load_ahead = [&](int t) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = NP - 1; i >= NP - AHEAD; --i) load_party(i % AHEAD, t, i);
+    };
+    __shared__ T by_row[TILE];
+    if (total) load_ahead(0);
+#pragma unroll 1
     for (int t = 0; t < total; ++t) {
         const bool second = t >= steps0;
         const Range<T> g = either(second, one.k, two.k);
         const Side<T> s = either(second, side0, side1);
         const int k0 = g.begin + (second ? t - steps0 : t) * kStep;
-        if (WEIGH == kByRow && !right && (t == 0 || t == steps0))              // the right factor's rows have no weights: none are looked up for them
-#pragma unroll
-            for (int half = 0; half < 2; ++half) by_row[half] = g.w ? g.w[min(s.along ? half * kRowsAtOnce + thread / 8 : lane, s.rows - 1) * g.stride] : g.same;
-        // What the words of the left factor count.
-        auto weigh = [&](T (&w)[kWords]) __attribute__((always_inline)) {
+        if (WEIGH == kByRow && threadIdx.x < TILE && (t == 0 || t == steps0))                  // (of a left wave)
+            by_row[threadIdx.x] = (g.w ? g.w[min((int)threadIdx.x, s.rows - 1) * g.stride] : 1) << g.shift;
+        const bool whole = k0 + kStep <= g.end && k0 + kStep - 1 <= g.below && k0 >= TILE - 1 + g.above;       // every word of the left factor counts
+        // What four words of the left factor count.
+        auto weigh = [&](T (&w)[4], int half) __attribute__((always_inline)) {
             if (right) return;
-            int u = thread;
-            asm volatile("" : "+v"(u));
+            if (WEIGH == kByRow)
 #pragma unroll
-            for (int e = 0; e < kWords; ++e) {
-                const int row = s.along ? e / 4 * kRowsAtOnce + u / 8 : u % 64, k = s.along ? k0 + u % 8 * 4 + e % 4 : k0 + quarter * kWords + e;
-                if (WEIGH == kByRow) w[e] *= by_row[e / 4];
-                if (WEIGH == kByK && g.w) w[e] *= ((const __attribute__((address_space(4))) T *)(uintptr_t)g.w)[min(k0 + quarter * kWords + e, s.ks - 1) * g.stride];
+                for (int e = 0; e < 4; ++e) w[e] *= by_row[row_of(s.along, half)];
+            if (whole) return;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int row = row_of(s.along, half), k = k0 + k_of(s.along, e);
                 w[e] = k < g.end && k <= row + g.below && k >= row + g.above ? w[e] : 0;
             }
         };
-        T open[kWords];
+        pair open[4];
 #pragma unroll
-        for (int e = 0; e < kWords; ++e) open[e] = 0;
+        for (int v = 0; v < 4; ++v) open[v] = pair{0, 0};
         __syncthreads();                                   // the last step's digits have been read
-        auto take = [&](const T (&value)[kWords], const T (&mask)[kWords], int i) __attribute__((always_inline)) {
+        // A party's words: its masks' digits, four words at a time.
+        auto take = [&](const pair (&value)[4], const pair (&mask)[4], int i) __attribute__((always_inline)) {
 #pragma unroll
-            for (int e = 0; e < kWords; ++e) open[e] += value[e] - mask[e];
-            if (i < GROUP) {
-                T w[kWords];
+            for (int v = 0; v < 4; ++v) open[v] += value[v] - mask[v];
+            if (i >= GROUP) return;
 #pragma unroll
-                for (int e = 0; e < kWords; ++e) w[e] = mask[e] + (i == 0 && right ? open[e] : 0);
-                weigh(w);
-                stage(w, 1 + i, s.along);
+            for (int half = 0; half < 2; ++half) {
+                T w[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) w[e] = word_of(mask, s.along, half, e);
+                if (i == 0 && right)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) w[e] += word_of(open, s.along, half, e);
+                weigh(w, half);
+                stage(w, half, 1 + i, s.along);
             }
-#pragma unroll
-            for (int e = 0; e < kWords; ++e) computed_here(open[e]);
         };
-        if constexpr (NP <= GROUP) {
+        if constexpr (AHEAD > 1) {
 #pragma unroll
             for (int i = NP - 1; i >= 0; --i) {
-                if (i) load_party((i - 1) % 2, t, i - 1);
-                __builtin_amdgcn_sched_barrier(0);         // one party's words under way, not all of them
-                take(x[i % 2], a[i % 2], i);
+                take(x[i % AHEAD], a[i % AHEAD], i);
+                __builtin_amdgcn_sched_barrier(0);         // these registers are another party's from here on
+                if (i >= AHEAD) load_party(i % AHEAD, t, i - AHEAD);
                 __builtin_amdgcn_sched_barrier(0);
             }
-        } else {
+        } else {                                           // a loop: the code is what short calls wait for first
 #pragma unroll 1
             for (int i = NP - 1; i >= 0; --i) {
-                load_party(0, t, i);
                 take(x[0], a[0], i);
+                load_party(0, i ? t : min(t + 1, total - 1), i ? i - 1 : NP - 1);
             }
         }
-        weigh(open);
-        stage(open, 0, s.along);
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {             // by k both opened factors are weighed, one in each product; the masks are not
+            T w[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) w[e] = word_of(open, s.along, half, e);
+            if (WEIGH == kByK && g.w)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) w[e] *= g.w[min(k0 + k_of(s.along, e), s.ks - 1) * g.stride];
+            weigh(w, half);
+            stage(w, half, 0, s.along);
+        }
         __builtin_amdgcn_sched_barrier(0);
-        if (NP <= GROUP && t + 1 < total) load_party((NP - 1) % 2, t + 1, NP - 1);
+        if (AHEAD > 1 && t + 1 < total) load_ahead(t + 1);
 #pragma unroll 1
         for (int first = 0;;) {
             __syncthreads();
@@ -263,32 +282,43 @@ template <int NP, class T, Weight WEIGH> __device__ inline void product_tile(con
             __syncthreads();
 #pragma unroll 1
             for (int i = 0; i < min(GROUP, NP - first); ++i) {
-                T w[kWords];
-                load(w, s, s.a + (first + i) * s.party, k0);
-                weigh(w);
-                stage(w, 1 + i, s.along);
+                pair w[4];
+                load(s, k0, first + i, true, w, w);
+#pragma unroll
+                for (int half = 0; half < 2; ++half) {
+                    T four[4];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) four[e] = word_of(w, s.along, half, e);
+                    weigh(four, half);
+                    stage(four, half, 1 + i, s.along);
+                }
             }
         }
     }
-    // The two halves' sums meet in LDS.
-    T *const sums = (T *)lds;
-    auto word = [&](int r) __attribute__((always_inline)) {
-        T v = 0;
-#pragma unroll
-        for (int d = ND - 1; d >= 0; --d) v = (v << 8) + (T)(std::make_signed_t<T>)acc[d][r];
-        return v;
-    };
+    // The waves' sums meet in LDS: of tiles of 64 those of one product in front of the other's, of tiles of 32 one product's in a part of its own.
     __syncthreads();
-    if (!right) {
+    constexpr int PARTS = TILE == 64 ? 1 : 2;
+    T *const to = (T *)lds + (right ? (PARTS - 1) * TILE * kPitch + (wm * 32 + lane % 32) * kPitch + wn * 32 + 4 * (lane / 32)
+                                    : (wm * 32 + 4 * (lane / 32)) * kPitch + wn * 32 + lane % 32);
+    const int stride = right ? 1 : kPitch, turn = TILE == 64 ? (right ? 1 : 0) : wave % 2;
+#pragma unroll 1
+    for (int half = 0; half < 2; ++half) {
+        if (turn == half) {
 #pragma unroll
-        for (int r = 0; r < 16; ++r) sums[(wm * 32 + 8 * (r / 4) + 4 * (lane / 32) + r % 4) * kPitch + wn * 32 + lane % 32] = word(r);
+            for (int r = 0; r < 16; ++r) {
+                T &sum = to[(8 * (r / 4) + r % 4) * stride];
+                sum = (half ? sum : 0) + word(r);
+                if (r % 4 == 3) __builtin_amdgcn_sched_barrier(0);
+            }
+        }
+        __syncthreads();
     }
-    __syncthreads();
-    if (right) {
-#pragma unroll
-        for (int r = 0; r < 16; ++r) sums[(wm * 32 + lane % 32) * kPitch + wn * 32 + 8 * (r / 4) + 4 * (lane / 32) + r % 4] += word(r);
-    }
-    __syncthreads();
+}
+// One of them.
+template <class T, int TILE> __device__ inline T sum_at(const char *lds, int row, int column)
+{
+    const T *s = (const T *)lds + row * (TILE + 1) + column;
+    return TILE == 64 ? s[0] : s[0] + s[TILE * (TILE + 1)];
 }
 
 // Which tile of which chunk (sequence and head before chunk) a workgroup has.  The tiles of a chunk read the same words: they are eight workgroup ids apart, on
@@ -313,139 +343,210 @@ __device__ inline Unit unit_of(const ChunkView &c, size_t unit)
     u.chunk = (int)(unit % c.chunks);
     u.b = (int)(u.head / c.heads);
     u.h = (int)(u.head % c.heads);
-    u.L = tokens_in(c, u.b, u.chunk);
+    u.L = tokens_in(c, c.lengths ? c.lengths[u.b] : c.tokens, u.chunk);
     return u;
 }
 constexpr int kEverywhere = 1 << 20;   // beyond all rows and k of a chunk
+
+// What is done with a tile's sums: a thread has one column of every eighth row.  The dealt words of kAtOnce rows are asked for together: one row after another
+// waits for memory every time.
+template <int NP, class T, int TILE, bool TUPLE> struct Rows {
+    static constexpr int kEach = TILE / 8, kWordsEach = TUPLE ? 4 * NP : 2 * NP, kMost = (sizeof(T) == 8 ? 96 : 32) / ((int)sizeof(T) / 4 * kWordsEach);
+    static constexpr int kAtOnce = kMost >= 4 ? 4 : kMost >= 2 ? 2 : 1, kRounds = kEach / kAtOnce;
+    const T *C;
+    Tuple<T> t;
+    size_t party, corner;              // words of a party, and where the tile starts
+    u32 pitch;
+    int rows, columns;                 // of the tile that there are
+    int below;                         // row i has columns up to i + below only: behind them its last word is read again
+    T c[kAtOnce][NP], r[kAtOnce][NP], top[kAtOnce][TUPLE ? NP : 1], msb[kAtOnce][TUPLE ? NP : 1];
+    static __device__ int column() { return threadIdx.x % TILE; }
+    static __device__ int row(int round, int k) { return (round * kAtOnce + k) * 8 + threadIdx.x / TILE; }
+    __device__ u32 offset(int row) const { return (u32)min(row, rows - 1) * pitch + (u32)min(min(column(), columns - 1), max(row + below, 0)); }
+    __device__ void load(int round)
+    {
+#pragma unroll
+        for (int k = 0; k < kAtOnce; ++k) {
+            const u32 at = offset(row(round, k));
+#pragma unroll
+            for (int i = 0; i < NP; ++i) {
+                const size_t from = i * party + corner;
+                c[k][i] = once(C + from + at), r[k][i] = once(t.r + from + at);
+                if (TUPLE) top[k][TUPLE ? i : 0] = once(t.r_top + from + at), msb[k][TUPLE ? i : 0] = once(t.r_msb + from + at);
+            }
+        }
+    }
+    __device__ T masked(int k, T z) const                  // what is opened of a result
+    {
+#pragma unroll
+        for (int i = 0; i < NP; ++i) z += c[k][i] + r[k][i];
+        return z;
+    }
+};
 template <class T> __device__ inline Segment<T> nothing_after(Segment<T> s)
 {
     s.k.begin = s.k.end;
     return s;
 }
 
-template <int NP, class T> __global__ __launch_bounds__(kProductBlock, 2) void scores_kernel(ScoresArgs<T> a)
+template <int NP, class T, int TILE> __global__ __launch_bounds__(kProductBlock<TILE>, (kProductOccupancy<NP, T, TILE>)) void scores_kernel(ScoresArgs<T> a)
 {
     extern __shared__ __align__(16) char lds[];
-    const int C = a.c.chunk, across = (C + kTile - 1) / kTile;
+    const int C = a.c.chunk, across = (C + TILE - 1) / TILE;
     const TileOf at = tile_of_workgroup(across * across);
     const size_t heads = (size_t)a.c.batch * a.c.heads;
     if (at.unit >= heads * a.c.chunks) return;
     const Unit u = unit_of(a.c, at.unit);
-    const int i0 = at.tile / across * kTile, j0 = at.tile % across * kTile;
+    const int i0 = at.tile / across * TILE, j0 = at.tile % across * TILE;
     const size_t each = heads * a.c.chunks * C * C, first = at.unit * C * C;
-    const bool any = j0 <= i0 && i0 < u.L;
-    if (any) {
-        const size_t party = heads * a.c.tokens * a.dim, token = u.head * a.c.tokens + (size_t)u.chunk * C;
-        const Segment<T> s{{a.x.x + (token + i0) * a.dim, a.x.a + (token + i0) * a.dim, party, (u32)a.dim, true, u.L - i0, a.dim},
-                           {a.y.x + (token + j0) * a.dim, a.y.a + (token + j0) * a.dim, party, (u32)a.dim, true, u.L - j0, a.dim},
-                           {0, a.dim, kEverywhere, -kEverywhere, nullptr, 0, 1}};
-        product_tile<NP, T, kNone>(s, nothing_after(s), lds);
-    }
-    for (int e = threadIdx.x; e < kTile * kTile; e += kProductBlock) {
-        const int r = e / kTile, d = e % kTile, i = i0 + r, j = j0 + d;
-        if (i >= C || j >= C) continue;
-        const size_t to = first + (size_t)i * C + j;
-        if (any && j <= i && i < u.L) {
-            finish<NP>(weight(a.decay, u.h, C, i - j) * ((const T *)lds)[r * kPitch + d], a.C, a.t, a.c.f + a.c.g, each, to, a.out);
-        } else {
+    if (j0 > i0 || i0 >= u.L) {                            // nothing of the tile is there
+        for (int e = threadIdx.x; e < TILE * TILE; e += kProductBlock<TILE>)
+            if (i0 + e / TILE < C && j0 + e % TILE < C)
 #pragma unroll
-            for (int k = 0; k < NP; ++k) a.out[k * each + to] = 0;
+                for (int k = 0; k < NP; ++k) a.out[k * each + first + (size_t)(i0 + e / TILE) * C + j0 + e % TILE] = 0;
+        return;
+    }
+    const size_t party = heads * a.c.tokens * a.dim, token = u.head * a.c.tokens + (size_t)u.chunk * C;
+    const Segment<T> s{{a.x.x + (token + i0) * a.dim, a.x.a + (token + i0) * a.dim, party, (u32)a.dim, true, u.L - i0, a.dim},
+                       {a.y.x + (token + j0) * a.dim, a.y.a + (token + j0) * a.dim, party, (u32)a.dim, true, u.L - j0, a.dim},
+                       {0, a.dim, kEverywhere, -kEverywhere, nullptr, 0, 0}};
+    product_tile<NP, T, TILE, kNone>(s, nothing_after(s), lds);
+    Rows<NP, T, TILE, true> rows{a.C, a.t, each, first + (size_t)i0 * C + j0, (u32)C, min(u.L, C) - i0, C - j0, i0 - j0};
+    rows.load(0);
+    const int d = rows.column(), j = j0 + d;
+#pragma unroll 1
+    for (int round = 0; round < rows.kRounds; ++round) {
+#pragma unroll
+        for (int k = 0; k < rows.kAtOnce; ++k) {
+            const int r = rows.row(round, k), i = i0 + r;
+            if (i >= C || j >= C) continue;
+            T *const to = a.out + rows.corner + (size_t)r * C + d;
+            const bool there = j <= i && i < u.L;
+            Opened<T> c{a.c.f + a.c.g};
+            if (there) c.add(rows.masked(k, weight(a.decay, u.h, C, i - j) * sum_at<T, TILE>(lds, r, d)));
+#pragma unroll
+            for (int p = 0; p < NP; ++p) to[p * each] = there ? c.truncated(p, rows.top[k][p], rows.msb[k][p]) : 0;
         }
+        if (round + 1 < rows.kRounds) rows.load(round + 1);
     }
 }
 
 // What is opened of a chunk's own part of the next state.
-template <int NP, class T> __global__ __launch_bounds__(kProductBlock, 2) void sums_kernel(StatesArgs<T> a)
+template <int NP, class T, int TILE> __global__ __launch_bounds__(kProductBlock<TILE>, (kProductOccupancy<NP, T, TILE>)) void sums_kernel(StatesArgs<T> a)
 {
     extern __shared__ __align__(16) char lds[];
-    const int C = a.c.chunk, across = (a.columns + kTile - 1) / kTile;
-    const TileOf at = tile_of_workgroup((a.rows + kTile - 1) / kTile * across);
+    const int C = a.c.chunk, across = (a.columns + TILE - 1) / TILE;
+    const TileOf at = tile_of_workgroup((a.rows + TILE - 1) / TILE * across);
     const size_t heads = (size_t)a.c.batch * a.c.heads, state = (size_t)a.rows * a.columns, each = heads * a.c.chunks * state;
     if (at.unit >= heads * a.c.chunks) return;
     const Unit u = unit_of(a.c, at.unit);
     if (u.L == 0) return;
-    const int r0 = at.tile / across * kTile, d0 = at.tile % across * kTile;
+    const int r0 = at.tile / across * TILE, d0 = at.tile % across * TILE;
     const size_t token = u.head * a.c.tokens + (size_t)u.chunk * C;
     const T *const w = a.decay ? a.decay + (size_t)u.h * (C + 1) + (a.reverse ? 1 : u.L - 1) : nullptr;
     const Segment<T> s{{a.x.x + token * a.rows + r0, a.x.a + token * a.rows + r0, heads * a.c.tokens * a.rows, (u32)a.rows, false, a.rows - r0, u.L},
                        {a.y.x + token * a.columns + d0, a.y.a + token * a.columns + d0, heads * a.c.tokens * a.columns, (u32)a.columns, false, a.columns - d0, u.L},
-                       {0, u.L, kEverywhere, -kEverywhere, w, a.reverse ? 1 : -1, 1}};
-    product_tile<NP, T, kByK>(s, nothing_after(s), lds);
-    for (int e = threadIdx.x; e < kTile * kTile; e += kProductBlock) {
-        const int r = e / kTile, d = e % kTile;
-        if (r0 + r >= a.rows || d0 + d >= a.columns) continue;
-        const size_t to = at.unit * state + (size_t)(r0 + r) * a.columns + d0 + d;
-        T z = ((const T *)lds)[r * kPitch + d];
+                       {0, u.L, kEverywhere, -kEverywhere, w, a.reverse ? 1 : -1, 0}};
+    product_tile<NP, T, TILE, kByK>(s, nothing_after(s), lds);
+    Rows<NP, T, TILE, false> rows{a.C, a.t, each, at.unit * state + (size_t)r0 * a.columns + d0, (u32)a.columns, min(TILE, a.rows - r0), min(TILE, a.columns - d0), kEverywhere};
+    rows.load(0);
+#pragma unroll 1
+    for (int round = 0; round < rows.kRounds; ++round) {
 #pragma unroll
-        for (int i = 0; i < NP; ++i) z += once(a.C + i * each + to) + once(a.t.r + i * each + to);
-        a.opened[to] = z;
+        for (int k = 0; k < rows.kAtOnce; ++k) {
+            const int r = rows.row(round, k), d = rows.column();
+            if (r < rows.rows && d < rows.columns) a.opened[rows.corner + (size_t)r * a.columns + d] = rows.masked(k, sum_at<T, TILE>(lds, r, d));
+        }
+        if (round + 1 < rows.kRounds) rows.load(round + 1);
     }
 }
 
-template <int NP, class T> __global__ __launch_bounds__(kProductBlock, 2) void outputs_kernel(OutputsArgs<T> a)
+template <int NP, class T, int TILE> __global__ __launch_bounds__(kProductBlock<TILE>, (kProductOccupancy<NP, T, TILE>)) void outputs_kernel(OutputsArgs<T> a)
 {
     extern __shared__ __align__(16) char lds[];
-    const int C = a.c.chunk, across = (a.columns + kTile - 1) / kTile;
-    const TileOf at = tile_of_workgroup((C + kTile - 1) / kTile * across);
+    const int C = a.c.chunk, across = (a.columns + TILE - 1) / TILE;
+    const TileOf at = tile_of_workgroup((C + TILE - 1) / TILE * across);
     const size_t heads = (size_t)a.c.batch * a.c.heads, each = heads * a.c.tokens * a.columns;
     if (at.unit >= heads * a.c.chunks) return;
     const Unit u = unit_of(a.c, at.unit);
-    const int i0 = at.tile / across * kTile, d0 = at.tile % across * kTile, there = min(C, a.c.tokens - u.chunk * C);
+    const int i0 = at.tile / across * TILE, d0 = at.tile % across * TILE, there = min(C, a.c.tokens - u.chunk * C);
     const size_t token = u.head * a.c.tokens + (size_t)u.chunk * C;
-    if (i0 < u.L) {
-        const size_t pairs = at.unit * C * C + (a.reverse ? i0 : (size_t)i0 * C), state = at.unit * a.rows * a.columns + (a.transposed ? (size_t)d0 * a.rows : d0);
-        const T *const w = a.decay ? a.decay + (size_t)u.h * (C + 1) + (a.reverse ? u.L - 1 - i0 : i0 + 1) : nullptr;
-        const Segment<T> own{{a.P.x + pairs, a.P.a + pairs, heads * a.c.chunks * C * C, (u32)C, !a.reverse, C - i0, C},
-                             {a.y.x + token * a.columns + d0, a.y.a + token * a.columns + d0, each, (u32)a.columns, false, a.columns - d0, u.L},
-                             {a.reverse ? i0 : 0, a.reverse ? u.L : min(u.L, i0 + kTile), a.reverse ? kEverywhere : i0, a.reverse ? i0 : -kEverywhere, nullptr, 0,
-                              (T)1 << a.c.g}};
-        const Segment<T> before{{a.x.x + (token + i0) * a.rows, a.x.a + (token + i0) * a.rows, heads * a.c.tokens * a.rows, (u32)a.rows, true, u.L - i0, a.rows},
-                                {a.S.x + state, a.S.a + state, heads * a.c.chunks * a.rows * a.columns, (u32)(a.transposed ? a.rows : a.columns), a.transposed,
-                                 a.columns - d0, a.rows},
-                                {0, a.rows, kEverywhere, -kEverywhere, w, a.reverse ? -1 : 1, 1}};
-        product_tile<NP, T, kByRow>(own, before, lds);
-    }
-#pragma unroll 1
-    for (int e = threadIdx.x; e < kTile * kTile; e += kProductBlock) {
-        const int r = e / kTile, d = e % kTile, i = i0 + r;
-        if (i >= there || d0 + d >= a.columns) continue;
-        const size_t to = (token + i) * a.columns + d0 + d;
-        if (i < u.L) {
-            finish<NP>(((const T *)lds)[r * kPitch + d], a.C, a.t, a.c.f + a.c.g, each, to, a.out);
-        } else {
+    if (i0 >= u.L) {
+        for (int e = threadIdx.x; e < TILE * TILE; e += kProductBlock<TILE>)
+            if (i0 + e / TILE < there && d0 + e % TILE < a.columns)
 #pragma unroll
-            for (int k = 0; k < NP; ++k) a.out[k * each + to] = 0;
+                for (int k = 0; k < NP; ++k) a.out[k * each + (token + i0 + e / TILE) * a.columns + d0 + e % TILE] = 0;
+        return;
+    }
+    const size_t pairs = at.unit * C * C + (a.reverse ? i0 : (size_t)i0 * C), state = at.unit * a.rows * a.columns + (a.transposed ? (size_t)d0 * a.rows : d0);
+    const T *const w = a.decay ? a.decay + (size_t)u.h * (C + 1) + (a.reverse ? u.L - 1 - i0 : i0 + 1) : nullptr;
+    const Segment<T> own{{a.P.x + pairs, a.P.a + pairs, heads * a.c.chunks * C * C, (u32)C, !a.reverse, C - i0, C},
+                         {a.y.x + token * a.columns + d0, a.y.a + token * a.columns + d0, each, (u32)a.columns, false, a.columns - d0, u.L},
+                         {a.reverse ? i0 : 0, a.reverse ? u.L : min(u.L, i0 + TILE), a.reverse ? kEverywhere : i0, a.reverse ? i0 : -kEverywhere, nullptr, 0, a.c.g}};
+    const Segment<T> before{{a.x.x + (token + i0) * a.rows, a.x.a + (token + i0) * a.rows, heads * a.c.tokens * a.rows, (u32)a.rows, true, u.L - i0, a.rows},
+                            {a.S.x + state, a.S.a + state, heads * a.c.chunks * a.rows * a.columns, (u32)(a.transposed ? a.rows : a.columns), a.transposed, a.columns - d0,
+                             a.rows},
+                            {0, a.rows, kEverywhere, -kEverywhere, w, a.reverse ? -1 : 1, 0}};
+    product_tile<NP, T, TILE, kByRow>(own, before, lds);
+    Rows<NP, T, TILE, true> rows{a.C, a.t, each, (token + i0) * a.columns + d0, (u32)a.columns, min(u.L, there) - i0, min(TILE, a.columns - d0), kEverywhere};
+    rows.load(0);
+    const int d = rows.column();
+#pragma unroll 1
+    for (int round = 0; round < rows.kRounds; ++round) {
+#pragma unroll
+        for (int k = 0; k < rows.kAtOnce; ++k) {
+            const int r = rows.row(round, k), i = i0 + r;
+            if (i >= there || d >= rows.columns) continue;
+            T *const to = a.out + rows.corner + (size_t)r * a.columns + d;
+            Opened<T> c{a.c.f + a.c.g};
+            c.add(rows.masked(k, sum_at<T, TILE>(lds, r, d)));
+#pragma unroll
+            for (int p = 0; p < NP; ++p) to[p * each] = i < u.L ? c.truncated(p, rows.top[k][p], rows.msb[k][p]) : 0;
         }
+        if (round + 1 < rows.kRounds) rows.load(round + 1);
     }
 }
 
-// From chunk to chunk, a thread an element of the state.
+// From chunk to chunk, a thread an element of the state: a stream of 3 NP + 1 words an element, those of kScanAtOnce chunks under way together.  Where a chunk has no tokens its
+// part of `opened` was not written: what is read of it is not used.
+template <int NP> constexpr int kScanAtOnce = NP <= 3 ? 4 : NP <= 6 ? 2 : 1;
 template <int NP, class T> __global__ __launch_bounds__(kBlock) void scan_kernel(StatesArgs<T> a)
 {
+    constexpr int AT_ONCE = kScanAtOnce<NP>;
     const int state = a.rows * a.columns, b = blockIdx.y / a.c.heads, h = blockIdx.y % a.c.heads, u = blockIdx.x * kBlock + threadIdx.x;
     if (u >= state) return;
     const size_t heads = (size_t)a.c.batch * a.c.heads, each = heads * a.c.chunks * state, one = heads * state;
+    const int length = a.c.lengths ? a.c.lengths[b] : a.c.tokens;
     T S[NP];
 #pragma unroll
     for (int i = 0; i < NP; ++i) S[i] = a.first ? a.first[i * one + (size_t)blockIdx.y * state + u] : 0;
-    for (int k = 0; k < a.c.chunks; ++k) {
-        const int chunk = a.reverse ? a.c.chunks - 1 - k : k, L = tokens_in(a.c, b, chunk);
-        const size_t at = ((size_t)blockIdx.y * a.c.chunks + chunk) * state + u;
-        T top[NP], msb[NP], old[NP];
-        Opened<T> c{a.c.f + a.c.g};
-        if (L) {
-            const T w = weight(a.decay, h, a.c.chunk, L) << a.c.f;
-            c.add(a.opened[at]);
+    for (int k0 = 0; k0 < a.c.chunks; k0 += AT_ONCE) {
+        T opened[AT_ONCE], top[AT_ONCE][NP], msb[AT_ONCE][NP], w[AT_ONCE];
+        size_t at[AT_ONCE];
+        int L[AT_ONCE];
 #pragma unroll
-            for (int i = 0; i < NP; ++i) c.add(w * S[i]), top[i] = a.t.r_top[i * each + at], msb[i] = a.t.r_msb[i * each + at];
+        for (int k = 0; k < AT_ONCE; ++k) {
+            const int step = min(k0 + k, a.c.chunks - 1), chunk = a.reverse ? a.c.chunks - 1 - step : step;
+            L[k] = tokens_in(a.c, length, chunk);
+            w[k] = weight(a.decay, h, a.c.chunk, L[k]) << a.c.f;
+            at[k] = ((size_t)blockIdx.y * a.c.chunks + chunk) * state + u;
+            opened[k] = once(a.opened + at[k]);
+#pragma unroll
+            for (int i = 0; i < NP; ++i) top[k][i] = once(a.t.r_top + i * each + at[k]), msb[k][i] = once(a.t.r_msb + i * each + at[k]);
         }
 #pragma unroll
-        for (int i = 0; i < NP; ++i) {
-            old[i] = S[i];
-            if (L) S[i] = c.truncated(i, top[i], msb[i]);
-        }
+        for (int k = 0; k < AT_ONCE; ++k) {
+            if (k0 + k >= a.c.chunks) break;
+            Opened<T> c{a.c.f + a.c.g};
+            c.add(opened[k]);
 #pragma unroll
-        for (int i = 0; i < NP; ++i) a.states[i * each + at] = old[i];
+            for (int i = 0; i < NP; ++i) {
+                c.add(w[k] * S[i]);
+                a.states[i * each + at[k]] = S[i];
+            }
+#pragma unroll
+            for (int i = 0; i < NP; ++i) S[i] = L[k] ? c.truncated(i, top[k][i], msb[k][i]) : S[i];
+        }
     }
 #pragma unroll
     for (int i = 0; i < NP; ++i) a.last[i * one + (size_t)blockIdx.y * state + u] = S[i];
@@ -525,13 +626,26 @@ template <int NP, class T> __global__ __launch_bounds__(kStepBlock) void step_ke
 }
 
 // Launches one of the kernels above on all tiles of all chunks.
-template <int NP, class T, class Kernel, class Args> inline spin_status launch_products(Kernel kernel, const Args &a, int tiles, OncePerDevice &lds_flags, hipStream_t s)
+template <int NP, class T, int TILE, class Kernel, class Args>
+inline spin_status launch_products(Kernel kernel, const Args &a, int rows, int columns, OncePerDevice &lds_flags, hipStream_t s)
 {
-    const spin_status st = allow_dynamic_lds((const void *)kernel, product_lds<NP, T>, lds_flags);
-    if (st == SPIN_OK) kernel<<<grid_of(workgroups(a.c, tiles)), kProductBlock, product_lds<NP, T>, s>>>(a);
+    const spin_status st = allow_dynamic_lds((const void *)kernel, product_lds<NP, T, TILE>, lds_flags);
+    const int tiles = ((rows + TILE - 1) / TILE) * ((columns + TILE - 1) / TILE);
+    if (st == SPIN_OK) kernel<<<grid_of(workgroups(a.c, tiles)), kProductBlock<TILE>, product_lds<NP, T, TILE>, s>>>(a);
     return st;
 }
-inline int tiles_of(int rows, int columns) { return ((rows + kTile - 1) / kTile) * ((columns + kTile - 1) / kTile); }
+// Tiles of 64 read and split every factor half as often, tiles of 32 are four times as many.  3 parties, 2 x 16 heads of 128, 4096 tokens in chunks of 128 (64-bit words): a prompt
+// 2.85 ms by 64, 3.24 by 32; 8 heads of 64, 300 tokens (40 tiles of 64): 102 us by 64, 66 by 32; 2 parties' training step of 16 heads of 64, 1024 tokens (256 tiles) 344
+// and 368.  32-bit words, which have fewer products to wait for: 24 heads of 80 and 48, chunks of 32, 125 us and 98.
+constexpr long kWantedTiles = 256;
+template <class T, class F> inline void for_tile(const ChunkView &c, int rows, int columns, F &&fn)
+{
+    if constexpr (sizeof(T) == 8) {
+        if (rows > 32 && columns > 32 && (long)c.batch * c.heads * c.chunks * ((rows + 63) / 64) * ((columns + 63) / 64) >= kWantedTiles)
+            return fn(std::integral_constant<int, 64>());
+    }
+    fn(std::integral_constant<int, 32>());
+}
 
 }  // namespace
 
@@ -540,9 +654,11 @@ template <class T> spin_status launch_linattn_scores(const ScoresArgs<T> &a, hip
     KernelTimer timer(SPIN_KERNEL_LINATTN, s);
     spin_status st = SPIN_OK;
     for_party_count(a.c.n, [&](auto np) {
-        constexpr int NP = decltype(np)::value;
-        static OncePerDevice lds_flags;
-        st = launch_products<NP, T>(scores_kernel<NP, T>, a, tiles_of(a.c.chunk, a.c.chunk), lds_flags, s);
+        for_tile<T>(a.c, a.c.chunk, a.c.chunk, [&](auto tile) {
+            constexpr int NP = decltype(np)::value, TILE = decltype(tile)::value;
+            static OncePerDevice lds_flags;
+            st = launch_products<NP, T, TILE>(scores_kernel<NP, T, TILE>, a, a.c.chunk, a.c.chunk, lds_flags, s);
+        });
     });
     return st != SPIN_OK ? st : check_launch("spin_linattn_scores");
 }
@@ -554,8 +670,11 @@ template <class T> spin_status launch_linattn_states(const StatesArgs<T> &a, hip
     spin_status st = SPIN_OK;
     for_party_count(a.c.n, [&](auto np) {
         constexpr int NP = decltype(np)::value;
-        static OncePerDevice lds_flags;
-        st = launch_products<NP, T>(sums_kernel<NP, T>, a, tiles_of(a.rows, a.columns), lds_flags, s);
+        for_tile<T>(a.c, a.rows, a.columns, [&](auto tile) {
+            constexpr int TILE = decltype(tile)::value;
+            static OncePerDevice lds_flags;
+            st = launch_products<NP, T, TILE>(sums_kernel<NP, T, TILE>, a, a.rows, a.columns, lds_flags, s);
+        });
         if (st == SPIN_OK) scan_kernel<NP, T><<<dim3(blocks, a.c.batch * a.c.heads), kBlock, 0, s>>>(a);
     });
     return st != SPIN_OK ? st : check_launch("spin_linattn_states");
@@ -566,9 +685,11 @@ template <class T> spin_status launch_linattn_outputs(const OutputsArgs<T> &a, h
     KernelTimer timer(SPIN_KERNEL_LINATTN, s);
     spin_status st = SPIN_OK;
     for_party_count(a.c.n, [&](auto np) {
-        constexpr int NP = decltype(np)::value;
-        static OncePerDevice lds_flags;
-        st = launch_products<NP, T>(outputs_kernel<NP, T>, a, tiles_of(a.c.chunk, a.columns), lds_flags, s);
+        for_tile<T>(a.c, a.c.chunk, a.columns, [&](auto tile) {
+            constexpr int NP = decltype(np)::value, TILE = decltype(tile)::value;
+            static OncePerDevice lds_flags;
+            st = launch_products<NP, T, TILE>(outputs_kernel<NP, T, TILE>, a, a.c.chunk, a.columns, lds_flags, s);
+        });
     });
     return st != SPIN_OK ? st : check_launch("spin_linattn_outputs");
 }

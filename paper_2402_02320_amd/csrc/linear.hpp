@@ -99,11 +99,10 @@ template <class T> __device__ inline void put(bool streamed, T *p, T v)
     else *p = v;
 }
 
-// Tokens of sequence b that are in a chunk.
-__host__ __device__ inline int tokens_in(const ChunkView &c, int b, int chunk)
+// Tokens of a sequence of `length` that are in a chunk.  The length may be anything.
+__host__ __device__ inline int tokens_in(const ChunkView &c, int length, int chunk)
 {
-    const int length = c.lengths ? c.lengths[b] : c.tokens, all = length < c.tokens ? length : c.tokens;
-    const int left = all - chunk * c.chunk;                // chunk * c.chunk < c.tokens
+    const int all = length < 0 ? 0 : length < c.tokens ? length : c.tokens, left = all - chunk * c.chunk;      // chunk * c.chunk < c.tokens
     return left < 0 ? 0 : left < c.chunk ? left : c.chunk;
 }
 
