@@ -24,7 +24,7 @@ template <int NP, class T, int WAVES, int EACH>
 __global__ __launch_bounds__(kNormBlock<WAVES>, WAVES > 4 ? 4 : 1) void norm_kernel(NormArgs<T> a, bool streamed)
 {
     constexpr int ROWS = kRowsAtOnce<WAVES>, THREADS = 64 * WAVES;
-    constexpr bool KEEP = NP * EACH * sizeof(T) <= 128;    // the masks stay in registers
+    constexpr bool KEEP = NP * EACH * sizeof(T) <= (WAVES > 4 ? 112 : 128);    // the masks stay in registers
     extern __shared__ __align__(16) char lds[];
     __shared__ T partial[ROWS][2][WAVES], shared[ROWS][NP + 2];
     const int slot = WAVES == 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x / 64) : 0, wave = WAVES == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x / 64);

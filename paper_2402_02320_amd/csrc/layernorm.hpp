@@ -85,9 +85,9 @@ template <class F> inline void for_dim(int dim, F &&fn)    // waves a row, words
     switch (norm_waves(dim)) {
     case 1: fn(std::integral_constant<int, 1>(), four); break;
     case 4: fn(four, four); break;
-    case 8: fn(std::integral_constant<int, 8>(), four); break;
     default:
-        if (dim <= 4096) fn(std::integral_constant<int, 16>(), four);
+        if (dim <= 2048) fn(std::integral_constant<int, 16>(), std::integral_constant<int, 2>());
+        else if (dim <= 4096) fn(std::integral_constant<int, 16>(), four);
         else fn(std::integral_constant<int, 16>(), std::integral_constant<int, 8>());
     }
 }

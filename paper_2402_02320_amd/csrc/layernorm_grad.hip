@@ -4,6 +4,9 @@
 namespace spin {
 namespace {
 
+__device__ inline void add_to(u64 *p, u64 v) { atomicAdd((unsigned long long *)p, (unsigned long long)v); }
+__device__ inline void add_to(u32 *p, u32 v) { atomicAdd(p, v); }
+
 // A wave's or workgroup's rows are `run` successive ones; its sums over them (of dgamma one word a column, since that is truncated, of dbeta a party's) stay in registers and are
 // added by a second kernel.
 // Where registers for those sums are not left (more parties, or words a thread: LEAN) columns_kernel makes them from memory, and no party's words are kept from one use to the next.
@@ -12,13 +15,12 @@ template <int NP, class T, int WAVES, int EACH>
 __global__ __launch_bounds__(kNormBlock<WAVES>, WAVES > 4 ? 4 : 1) void norm_grad_kernel(NormGradArgs<T> a, int run, T *sums, bool streamed)
 {
     constexpr int ROWS = kRowsAtOnce<WAVES>, THREADS = 64 * WAVES;
-    constexpr bool LEAN = kLean<NP, T, WAVES, EACH>, KEEP = !LEAN && 2 * NP * EACH * sizeof(T) <= (WAVES > 4 ? 64 : 128);
+    constexpr bool LEAN = kLean<NP, T, WAVES, EACH>, KEEP = !LEAN && 2 * NP * EACH * sizeof(T) <= (WAVES > 4 ? 96 : 128);
     __shared__ T partial[ROWS][2][WAVES], shared[ROWS][3 * NP + 2], words_of[ROWS][(kNormGradWords + 1) * NP];
     const int slot = WAVES == 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x / 64) : 0, wave = WAVES == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     const int t = threadIdx.x % THREADS;
-    const long group = (long)blockIdx.x * ROWS + slot;
+    const long group = (long)blockIdx.x * ROWS + slot;     // of rows: a wave's or workgroup's
     const long row0 = group * run, row1 = min(row0 + run, (long)a.rows);
-    if (row0 >= row1) return;                              // of a whole wave or workgroup
     const size_t party = (size_t)a.rows * a.dim;
     T *const words = words_of[slot];
     const Chain<NP, T> chain{words};
@@ -131,15 +133,32 @@ __global__ __launch_bounds__(kNormBlock<WAVES>, WAVES > 4 ? 4 : 1) void norm_gra
         }
         row_barrier<WAVES>();
     }
-    if (LEAN) return;
+    if constexpr (!LEAN) {
+        T *const to = sums + (size_t)blockIdx.x * (NP + 1) * a.dim;
+        if constexpr (WAVES == 1) {                        // four waves' sums first meet in LDS
+            __shared__ T room[(NP + 1) * THREADS * EACH];
+            for (int k = threadIdx.x; k < (NP + 1) * a.dim; k += kNormBlock<WAVES>) room[k] = 0;
+            __syncthreads();
 #pragma unroll
-    for (int j = 0; j < EACH; ++j) {
-        const int d = j * THREADS + t;
-        if (d >= a.dim) break;
-        T *const to = sums + group * (NP + 1) * a.dim + d;
-        to[0] = gamma_sum[LEAN ? 0 : j];
+            for (int j = 0; j < EACH; ++j) {
+                const int d = j * THREADS + t;
+                if (d >= a.dim) break;
+                add_to(&room[d], gamma_sum[j]);
 #pragma unroll
-        for (int i = 0; i < NP; ++i) to[(size_t)(1 + i) * a.dim] = beta_sum[LEAN ? 0 : j][i];
+                for (int i = 0; i < NP; ++i) add_to(&room[(1 + i) * a.dim + d], beta_sum[j][i]);
+            }
+            __syncthreads();
+            for (int k = threadIdx.x; k < (NP + 1) * a.dim; k += kNormBlock<WAVES>) to[k] = room[k];
+        } else {
+#pragma unroll
+            for (int j = 0; j < EACH; ++j) {
+                const int d = j * THREADS + t;
+                if (d >= a.dim) break;
+                to[d] = gamma_sum[j];
+#pragma unroll
+                for (int i = 0; i < NP; ++i) to[(size_t)(1 + i) * a.dim + d] = beta_sum[j][i];
+            }
+        }
     }
 }
 
@@ -211,12 +230,13 @@ template <int NP, class T> __global__ __launch_bounds__(kJoinBlock) void join_ke
     for (int i = 0; i < NP; ++i) a.dgamma[(size_t)i * a.dim + d] = c.truncated(i, top[i], msb[i]);
 }
 
-// Of the backward pass: rows of one wave or workgroup, and how many of those there are.
-struct Runs { int run; long groups; };
+// Rows of one wave or workgroup, and how many groups of rows have sums of their own: those of a workgroup.
+struct Runs { int run, groups; };
 inline Runs runs_of(int rows, int dim)
 {
-    const int wanted = dim <= 256 ? 4096 : dim <= 1024 ? 1024 : 512, run = (rows + wanted - 1) / wanted;
-    return {run, ((long)rows + run - 1) / run};
+    const int waves = norm_waves(dim), at_once = waves == 1 ? 4 : 1, wanted = waves == 1 ? 1024 : waves == 4 ? 1024 : 256;
+    const int run = (int)(((long)rows + (long)wanted * at_once - 1) / ((long)wanted * at_once));
+    return {run, (int)(((long)rows + (long)run * at_once - 1) / ((long)run * at_once))};
 }
 
 }  // namespace
@@ -233,9 +253,9 @@ template <class T> spin_status launch_layernorm_grad(const NormGradArgs<T> &a, h
         constexpr int NP = decltype(np)::value;
         for_dim(a.dim, [&](auto waves, auto each) {
             constexpr int WAVES = decltype(waves)::value, ROWS = kRowsAtOnce<WAVES>;
-            norm_grad_kernel<NP, T, WAVES, decltype(each)::value><<<(unsigned)((r.groups + ROWS - 1) / ROWS), kNormBlock<WAVES>, 0, s>>>(a, r.run, sums, streamed);
+            norm_grad_kernel<NP, T, WAVES, decltype(each)::value><<<r.groups, kNormBlock<WAVES>, 0, s>>>(a, r.run, sums, streamed);
             if constexpr (kLean<NP, T, WAVES, decltype(each)::value>)
-                columns_kernel<NP, T><<<dim3((a.dim + 63) / 64, (unsigned)r.groups), 64 * kColumnRows, 0, s>>>(a, r.run, sums);
+                columns_kernel<NP, T><<<dim3((a.dim + 63) / 64, r.groups), 64 * kColumnRows, 0, s>>>(a, r.run * ROWS, sums);
         });
         join_kernel<NP, T><<<dim3((a.dim + kJoinColumns - 1) / kJoinColumns, NP + 1), kJoinBlock, 0, s>>>(a, r.groups, sums);
     });

@@ -84,7 +84,7 @@ size_t layernorm_grad_workspace(int n, int rows, int dim, int word_bytes);
 
 constexpr int kNormWords = 15, kNormGradWords = 22;        // of a row: a Newton step's (and as many besides), the gradient's
 constexpr int kMostDim = 8192;
-constexpr int norm_waves(int dim) { return dim <= 256 ? 1 : dim <= 1024 ? 4 : dim <= 2048 ? 8 : 16; }       // of a row
+constexpr int norm_waves(int dim) { return dim <= 256 ? 1 : dim <= 1024 ? 4 : 16; }       // of a row
 
 namespace {
 
