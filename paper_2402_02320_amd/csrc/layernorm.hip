@@ -154,7 +154,7 @@ template <class T> spin_status launch_layernorm(const NormArgs<T> &a, hipStream_
     const bool streamed = (size_t)a.n * a.rows * a.dim * sizeof(T) >= kStreamingBytes;
     spin_status st = SPIN_OK;
     for_party_count(a.n, [&](auto np) {
-        for_dim(a.dim, [&](auto waves, auto each) {
+        for_dim(a.rows, a.dim, [&](auto waves, auto each) {
             constexpr int NP = decltype(np)::value, WAVES = decltype(waves)::value, ROWS = kRowsAtOnce<WAVES>;
             constexpr auto kernel = norm_kernel<NP, T, WAVES, decltype(each)::value>;
             constexpr int row_bytes = kNormWords * NP * (int)sizeof(T) * ROWS;

@@ -79,10 +79,10 @@ __device__ inline void make_new(u32 &column)
     asm volatile("" : "+v"(column));
 }
 
-template <class F> inline void for_dim(int dim, F &&fn)    // waves a row, words a thread
+template <class F> inline void for_dim(int rows, int dim, F &&fn)    // waves a row, words a thread
 {
     const std::integral_constant<int, 4> four;
-    switch (norm_waves(dim)) {
+    switch (norm_waves(rows, dim)) {
     case 1: fn(std::integral_constant<int, 1>(), four); break;
     case 4: fn(four, four); break;
     default:

@@ -234,7 +234,7 @@ template <int NP, class T> __global__ __launch_bounds__(kJoinBlock) void join_ke
 struct Runs { int run, groups; };
 inline Runs runs_of(int rows, int dim)
 {
-    const int waves = norm_waves(dim), at_once = waves == 1 ? 4 : 1, wanted = waves == 1 ? 1024 : waves == 4 ? 1024 : 256;
+    const int waves = norm_waves(rows, dim), at_once = waves == 1 ? 4 : 1, wanted = waves == 1 ? 1024 : waves == 4 ? 1024 : 256;
     const int run = (int)(((long)rows + (long)wanted * at_once - 1) / ((long)wanted * at_once));
     return {run, (int)(((long)rows + (long)run * at_once - 1) / ((long)run * at_once))};
 }
@@ -251,7 +251,7 @@ template <class T> spin_status launch_layernorm_grad(const NormGradArgs<T> &a, h
     T *const sums = (T *)a.workspace;
     for_party_count(a.n, [&](auto np) {
         constexpr int NP = decltype(np)::value;
-        for_dim(a.dim, [&](auto waves, auto each) {
+        for_dim(a.rows, a.dim, [&](auto waves, auto each) {
             constexpr int WAVES = decltype(waves)::value, ROWS = kRowsAtOnce<WAVES>;
             norm_grad_kernel<NP, T, WAVES, decltype(each)::value><<<r.groups, kNormBlock<WAVES>, 0, s>>>(a, r.run, sums, streamed);
             if constexpr (kLean<NP, T, WAVES, decltype(each)::value>)

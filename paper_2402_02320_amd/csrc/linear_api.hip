@@ -106,7 +106,7 @@ spin_status check_norm(const spin_norm *s, int most)
 {
     if (s == nullptr || bad_n(s->n) || s->rows < 1 || s->dim < 1 || s->dim > kMostDim || s->f < 1 || s->f >= most || s->shift < 1 || s->shift > most) return SPIN_EINVAL;
     // a launch has fewer than 2^32 threads
-    if (s->rows > (1 << 24) || (double)s->rows * norm_waves(s->dim) * 64 > (double)(1u << 31)) return SPIN_ERANGE;
+    if (s->rows > (1 << 24) || (double)s->rows * norm_waves(s->rows, s->dim) * 64 > (double)(1u << 31)) return SPIN_ERANGE;
     return (double)s->n * s->rows * s->dim > kMaxWords ? SPIN_ERANGE : SPIN_OK;
 }
 
