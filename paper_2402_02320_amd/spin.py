@@ -968,9 +968,8 @@ class _Word:
         """The library's description of the heads and their chunks."""
         if decay is None and g:
             raise SpinError("without a decay there are no fractional bits g of it")
-        for t in (decay, lengths):
-            if t is not None:
-                _on_this_device(t, name)
+        if lengths is not None:
+            _on_this_device(lengths, name)
         return ctypes.byref(_LinAttn(*_ints(n, batch, heads, tokens, chunk, f, g), None if decay is None else self._of(decay, "decay", heads, chunk + 1),
                                      None if lengths is None else _list32(lengths, name, batch)))
 

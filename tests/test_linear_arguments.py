@@ -1,0 +1,261 @@
+"""What the calls of linear attention and layer norm refuse, on the CPU: the C entry points before any launch, and the Python binding before the library."""
+import ctypes
+
+import pytest
+import torch
+
+from paper_2402_02320_amd import spin
+from test_binding_arguments import Workspace, record, w  # noqa: F401  (a fixture)
+
+
+
+class Space(Workspace):
+    def get_device(self): return 0
+
+
+WS = Space()
+EINVAL, ERANGE, EWORKSPACE = 1, 2, 3
+P, ODD = 0x10000, 0x10008
+RINGS = pytest.mark.parametrize("pre,most", [("spin_", 61), ("spin32_", 29)])
+
+
+@pytest.fixture(scope="module")
+def L():
+    return spin.lib()
+
+
+def heads(**kw):
+    d = dict(n=2, batch=2, heads=3, tokens=100, chunk=64, f=9, g=6, decay=P, lengths=P)
+    d.update(kw)
+    return ctypes.byref(spin._LinAttn(*[d[k] for k, _ in spin._LinAttn._fields_]))
+
+
+def masked(value=P, mask=P):
+    return ctypes.byref(spin._Masked(value, mask))
+
+
+def dealt(*r):
+    return ctypes.byref(spin._Tuple(*(r or (P, P, P))))
+
+
+def norm(**kw):
+    d = dict(n=2, rows=7, dim=33, f=9, shift=15)
+    d.update(kw)
+    return ctypes.byref(spin._Norm(*[d[k] for k, _ in spin._Norm._fields_]))
+
+
+BAD_POINTERS = (None, ODD)
+BAD_FACTORS = [None] + [masked(*p) for p in ((None, P), (P, None), (ODD, P), (P, ODD))]
+BAD_TUPLES = [None] + [dealt(*[bad if k == i else P for k in range(3)]) for i in range(3) for bad in BAD_POINTERS]
+
+
+def bad_heads(most, chunks):
+    for kw in (dict(n=0), dict(n=9), dict(batch=0), dict(heads=-1), dict(f=0), dict(f=most + 1, g=0), dict(g=-1), dict(f=most - 5), dict(f=2 ** 31 - 1, g=2 ** 31 - 1),
+               dict(decay=None), dict(decay=ODD), dict(lengths=P + 2)):
+        yield kw, EINVAL
+    yield dict(batch=20000, heads=4), ERANGE
+    if chunks:
+        for kw in (dict(tokens=0), dict(tokens=-1), dict(chunk=0), dict(chunk=16), dict(chunk=96), dict(chunk=256), dict(chunk=-64)):
+            yield kw, EINVAL
+        yield dict(tokens=(1 << 24) + 1), ERANGE
+        yield dict(tokens=2 ** 31 - 1), ERANGE
+        yield dict(batch=1, heads=65000, tokens=1 << 24), ERANGE
+
+
+def each_bad(calls, good):
+    """calls: argument -> what it must not be; everything else as in `good`."""
+    for k, bads in calls.items():
+        for bad in bads:
+            yield [bad if i == k else v for i, v in enumerate(good)]
+
+
+@RINGS
+def test_refusals_of_chunked_attention(L, pre, most):
+    sc, st, ou, need = (getattr(L, pre + "linattn_" + k) for k in ("scores", "states", "outputs", "states_workspace_bytes"))
+    good_sc = [heads(), 64, masked(), masked(), P, dealt(), P, None]
+    good_st = [heads(), 64, 40, 0, masked(), masked(), P, dealt(), P, P, P, P, 1 << 40, None]
+    good_ou = [heads(), 64, 40, 0, 0, masked(), masked(), masked(), masked(), P, dealt(), P, None]
+    for kw, bad in bad_heads(most, True):
+        for fn, good in ((sc, good_sc), (st, good_st), (ou, good_ou)):
+            assert fn(heads(**kw), *good[1:]) == bad, kw
+        assert need(heads(**kw), 64, 40) == 0, kw
+    for fn, good in ((sc, good_sc), (st, good_st), (ou, good_ou)):
+        assert fn(None, *good[1:]) == EINVAL
+    dims = (0, -8, 4, 12, 264, 2 ** 31 - 8)
+    for args in each_bad({1: dims, 2: BAD_FACTORS, 3: BAD_FACTORS, 4: BAD_POINTERS, 5: BAD_TUPLES, 6: BAD_POINTERS}, good_sc):
+        assert sc(*args) == EINVAL, args
+    for args in each_bad({1: dims, 2: dims, 4: BAD_FACTORS, 5: BAD_FACTORS, 6: BAD_POINTERS, 7: BAD_TUPLES, 8: (ODD,), 9: BAD_POINTERS, 10: BAD_POINTERS}, good_st):
+        assert st(*args) == EINVAL, args
+    for args in each_bad({1: dims, 2: dims, 5: BAD_FACTORS, 6: BAD_FACTORS, 7: BAD_FACTORS, 8: BAD_FACTORS, 9: BAD_POINTERS, 10: BAD_TUPLES, 11: BAD_POINTERS}, good_ou):
+        assert ou(*args) == EINVAL, args
+    size = need(heads(), 64, 40)
+    assert size == 2 * 3 * 2 * 64 * 40 * (8 if pre == "spin_" else 4)
+    for args in each_bad({11: (None, P + 128), 12: (size - 1, 0)}, good_st):
+        assert st(*args) == EWORKSPACE, args
+    for d in dims:
+        assert need(heads(), d, 40) == need(heads(), 64, d) == 0
+
+
+@RINGS
+def test_refusals_of_a_step(L, pre, most):
+    step = getattr(L, pre + "linattn_step")
+    good = [heads(tokens=0, chunk=0), 64, 40, P, masked(), masked(), masked(), P, P, dealt(), P, dealt(), P, P, None]
+    for kw, bad in bad_heads(most, False):
+        assert step(heads(**kw), *good[1:]) == bad, kw
+    dims = (0, -8, 4, 12, 264)
+    for args in each_bad({0: (None,), 1: dims, 2: dims, 3: BAD_POINTERS, 4: BAD_FACTORS, 5: BAD_FACTORS, 6: BAD_FACTORS, 7: BAD_POINTERS, 8: BAD_POINTERS, 9: BAD_TUPLES,
+                          10: BAD_POINTERS, 11: BAD_TUPLES, 12: BAD_POINTERS, 13: BAD_POINTERS}, good):
+        assert step(*args) == EINVAL, args
+
+
+@RINGS
+def test_refusals_of_the_norm(L, pre, most):
+    fwd, bwd, need, need_grad = (getattr(L, pre + "layernorm" + k) for k in ("", "_grad", "_workspace_bytes", "_grad_workspace_bytes"))
+    good = [norm(), 3, 1, 2, 3, P, masked(), P, P, P, P, dealt(), P, dealt(), P, P, P, P, P, 1 << 40, None]
+    back = [norm(), masked(), masked(), P, masked(), P, P, dealt(), P, dealt(), P, P, P, P, P, P, 1 << 40, None]
+    for kw, bad in [(dict(n=0), EINVAL), (dict(n=9), EINVAL), (dict(rows=0), EINVAL), (dict(rows=-3), EINVAL), (dict(dim=0), EINVAL), (dict(dim=8193), EINVAL), (dict(f=0), EINVAL),
+                    (dict(f=most), EINVAL), (dict(shift=0), EINVAL), (dict(shift=most + 1), EINVAL), (dict(rows=(1 << 24) + 1), ERANGE), (dict(rows=1 << 22, dim=8192), ERANGE),
+                    (dict(rows=2 ** 31 - 1), ERANGE)]:
+        assert fwd(norm(**kw), *good[1:]) == bwd(norm(**kw), *back[1:]) == bad, kw
+        assert need(norm(**kw)) == need_grad(norm(**kw)) == 0, kw
+    assert need(None) == need_grad(None) == 0
+    for args in each_bad({0: (None,), 1: (-1, 17), 5: BAD_POINTERS, 6: BAD_FACTORS, 7: BAD_POINTERS, 8: BAD_POINTERS, 9: BAD_POINTERS, 10: BAD_POINTERS, 11: BAD_TUPLES,
+                          12: BAD_POINTERS, 13: BAD_TUPLES, 14: BAD_POINTERS, 15: BAD_POINTERS, 16: (ODD,), 17: (ODD,)}, good):
+        assert fwd(*args) == EINVAL, args
+    for args in each_bad({0: (None,), 1: BAD_FACTORS, 2: BAD_FACTORS, 3: BAD_POINTERS, 4: BAD_FACTORS, 5: BAD_POINTERS, 6: BAD_POINTERS, 7: BAD_TUPLES, 8: BAD_POINTERS,
+                          9: BAD_TUPLES, 10: BAD_POINTERS, 11: BAD_POINTERS, 12: BAD_POINTERS, 13: BAD_POINTERS, 14: BAD_POINTERS}, back):
+        assert bwd(*args) == EINVAL, args
+    for args in each_bad({18: (None, P + 64), 19: (need(norm()) - 1,)}, good):
+        assert fwd(*args) == EWORKSPACE, args
+    for args in each_bad({15: (None, P + 64), 16: (need_grad(norm()) - 1,)}, back):
+        assert bwd(*args) == EWORKSPACE, args
+
+
+# ---- the binding ----------------------------------------------------------------------------------------------
+def values(*shape):
+    return w(2, 1, 3, *shape)
+
+
+def pair(*shape):
+    return (values(*shape), values(*shape))
+
+
+def cut(*shape):
+    return [values(*shape) for _ in range(3)]
+
+
+class Lists:
+    """In place of torch.int32 CUDA lists, and of a GPU."""
+
+    def __init__(self, monkeypatch):
+        monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+        monkeypatch.setattr(spin, "_list32", lambda t, name, *shape: spin._shapes(tuple(t.shape) == shape) or 1)
+
+
+DECAY = torch.zeros(3, 33, dtype=torch.int64)
+SCORES = dict(x=pair(40, 8), y=pair(40, 8), C=values(2, 32, 32), tuple_=cut(2, 32, 32), f=9, decay=DECAY, g=6, lengths=torch.zeros(1, dtype=torch.int32))
+STATES = dict(x=pair(40, 8), y=pair(40, 16), C=values(2, 8, 16), tuple_=cut(2, 8, 16), f=9, chunk=32, decay=DECAY, g=6, first=values(8, 16), workspace=WS)
+OUTPUTS = dict(P=pair(2, 32, 32), y=pair(40, 16), x=pair(40, 8), S=pair(2, 8, 16), C=values(40, 16), tuple_=cut(40, 16), f=9, decay=DECAY, g=6)
+STEP = dict(S=values(8, 16), q=pair(8), k=pair(8), v=pair(16), mask=values(8, 16), C=(values(8, 16), values(16)), tuples=(cut(8, 16), cut(16)), f=9,
+            decay=torch.zeros(3, 2, dtype=torch.int64), g=6, active=torch.zeros(1, dtype=torch.int32))
+
+
+def rows(*shape):
+    return w(2, *shape)
+
+
+NORM = dict(x=rows(5, 7), gamma=(rows(7), rows(7)), beta=rows(7), masks=(rows(5, 7),) * 2, C=(rows(5, 7),) * 2, tuples=([rows(5, 7)] * 3,) * 2, row_words=rows(45, 5), f=9, shift=15,
+            line=(3, 2), workspace=WS)
+GRAD = dict(dy=rows(5, 7), xhat=rows(5, 7), rstd=rows(5), gamma=(rows(7), rows(7)), masks=(rows(5, 7),) * 3, C=(rows(5, 7),) * 2, tuples=([rows(5, 7)] * 3,) * 2,
+            row_words=rows(22, 5), column_words=rows(4, 7), f=9, shift=15, workspace=WS)
+CALLS = {"linattn_scores": (SCORES, values(2, 32, 32)), "linattn_states": (STATES, (values(2, 8, 16), values(8, 16))), "linattn_outputs": (OUTPUTS, values(40, 16)),
+         "linattn_step": (STEP, (values(16), values(8, 16))), "layernorm": (NORM, (rows(5, 7), rows(5, 7), rows(5))), "layernorm_grad": (GRAD, (rows(5, 7), rows(7), rows(7)))}
+
+
+def longer(v):
+    """Every way in which one tensor within v has another shape (a row more of its last axis, or of its first)."""
+    if isinstance(v, torch.Tensor):
+        yield torch.cat([v, v[..., :1]], -1)
+        yield torch.cat([v, v[:1]], 0)
+    elif isinstance(v, (tuple, list)) and any(isinstance(k, (torch.Tensor, tuple, list)) for k in v):
+        for i, one in enumerate(v):
+            for other in longer(one):
+                yield type(v)([other if k == i else o for k, o in enumerate(v)])
+        yield v[:-1]                                          # and one operand too few
+
+
+@pytest.mark.parametrize("name", sorted(CALLS))
+def test_operands_of_other_shapes_reach_no_kernel(name, record, monkeypatch):  # noqa: F811
+    Lists(monkeypatch)
+    good, _ = CALLS[name]
+    call = getattr(spin, name)
+    tried = 0
+    for k, v in good.items():
+        if k in ("workspace", "line"):
+            continue
+        for other in longer(v):
+            with pytest.raises((spin.SpinError, ValueError, IndexError)):
+                call(**dict(good, **{k: other}))
+            tried += 1
+    assert tried > 12 and record.launched == []
+    call(**good)
+    assert record.launched == ["spin_" + name]
+
+
+@pytest.mark.parametrize("name", sorted(CALLS))
+def test_results_that_are_too_short_reach_no_kernel(name, record, monkeypatch):  # noqa: F811
+    Lists(monkeypatch)
+    good, out = CALLS[name]
+    call = getattr(spin, name)
+    outs = out if isinstance(out, tuple) else (out,)
+    for i, t in enumerate(outs):
+        short = [torch.empty(t.numel() - 1, dtype=torch.int64) if k == i else o for k, o in enumerate(outs)]
+        with pytest.raises(spin.SpinError):
+            call(**good, out=tuple(short) if isinstance(out, tuple) else short[0])
+    assert record.launched == []
+    call(**good, out=out)
+    assert len(record.launched) == 1
+
+
+def test_a_precision_without_a_decay_is_refused(record, monkeypatch):  # noqa: F811
+    Lists(monkeypatch)
+    for name in ("linattn_scores", "linattn_outputs", "linattn_step"):
+        with pytest.raises(spin.SpinError, match="without a decay"):
+            getattr(spin, name)(**dict(CALLS[name][0], decay=None))
+    assert record.launched == []
+
+
+def test_numbers_past_32_bits_are_refused(record, monkeypatch):  # noqa: F811
+    Lists(monkeypatch)
+    for name, key in (("linattn_scores", "f"), ("linattn_states", "chunk"), ("linattn_outputs", "g"), ("linattn_step", "f"), ("layernorm", "shift"), ("layernorm_grad", "f")):
+        with pytest.raises(spin.SpinError):
+            getattr(spin, name)(**dict(CALLS[name][0], **{key: (1 << 32) + 9}))
+    assert record.launched == []
+
+
+def test_tensors_of_another_device_are_refused(record, monkeypatch):  # noqa: F811
+    class Elsewhere:
+        is_cuda = True
+
+        def get_device(self): return 1
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    with pytest.raises(spin.SpinError, match="device 1"):
+        spin._on_this_device(Elsewhere(), "x")
+    Lists(monkeypatch)
+    seen = []
+    monkeypatch.setattr(spin, "_on_this_device", lambda t, name: seen.append(name))
+    for name, (good, out) in CALLS.items():
+        getattr(spin, name)(**good, out=out)
+    # every tensor of every call is looked at
+    assert len(seen) == sum(len(list(tensors(good))) + len(list(tensors(out))) + ("workspace" in good) for good, out in CALLS.values())
+
+
+def tensors(v):
+    if isinstance(v, torch.Tensor):
+        yield v
+    elif isinstance(v, (tuple, list)):
+        for k in v:
+            yield from tensors(k)
+    elif isinstance(v, dict):
+        for k in v.values():
+            yield from tensors(k)
