@@ -502,13 +502,12 @@ typedef struct {
  * so 1 / sqrt(v) is Newton's, from the public line offset - slope v (ring words at f bits); it converges where that first guess y has 0 < v y^2 < 3.
  * The words 3, k+1, k+6, k+11 and C1, C2 are the dealt shares of the masks' products.  x, mask_x, mask_xhat, C1, C2, t1, t2, out, xhat: [n][rows][dim]; gamma, beta:
  * [n][dim]; rstd: [n][rows].  xhat and rstd, which the gradient takes, may be NULL.  out may alias C2 or an array of t2, xhat C1 or one of t1.
- * 0 <= iterations <= 16.  workspace: device scratch of spin_layernorm_workspace_bytes() bytes (0 if the arguments are invalid), 256-byte aligned.     */
+ * 0 <= iterations <= 16.                                                                                                                       */
 #define SPIN_MAX_NORM_ITERATIONS 16
 spin_status spin_layernorm(const spin_norm *s, int iterations, uint64_t offset, uint64_t slope, uint64_t eps, const uint64_t *x,
                            const spin_masked *gamma, const uint64_t *beta, const uint64_t *mask_x, const uint64_t *mask_xhat,
                            const uint64_t *C1, const spin_tuple *t1, const uint64_t *C2, const spin_tuple *t2, const uint64_t *row_words,
-                           uint64_t *out, uint64_t *xhat, uint64_t *rstd, void *workspace, size_t workspace_bytes, spin_stream stream);
-size_t spin_layernorm_workspace_bytes(const spin_norm *s);
+                           uint64_t *out, uint64_t *xhat, uint64_t *rstd, spin_stream stream);
 
 /* Gradients from dy, that of the result.  column_words: [n][4][dim]; row_words: [n][22][rows], t(k) as above:
  *     g      = T(C1 + dy gamma, f), t1;   dy, xhat and g are opened against their masks
@@ -517,7 +516,8 @@ size_t spin_layernorm_workspace_bytes(const spin_norm *s);
  *     k1 = T(word 12 + m1 rstd, f), m1 against word 11, t(13);   k2 = T(word 17 + m2 rstd, f), m2 against word 16, t(18);   k2 is opened against word 21
  *     dx = T(C2 + g rstd - xhat k2, f) - k1, t2
  * Column word 0, words 3, 12, 17 and C1, C2 (of g rstd - xhat k2) are the dealt shares of the masks' products.  dy, xhat, C1, C2, t1, t2, dx: [n][rows][dim]; gamma, dgamma,
- * dbeta: [n][dim]; rstd: [n][rows].  xhat's mask may be the forward pass's.  dx may alias C2 or an array of t2.  workspace as above.                              */
+ * dbeta: [n][dim]; rstd: [n][rows].  xhat's mask may be the forward pass's.  dx may alias C2 or an array of t2.  workspace: device scratch of
+ * spin_layernorm_grad_workspace_bytes() bytes (0 if the arguments are invalid), 256-byte aligned.                                                  */
 spin_status spin_layernorm_grad(const spin_norm *s, const spin_masked *dy, const spin_masked *xhat, const uint64_t *rstd, const spin_masked *gamma,
                                 const uint64_t *mask_g, const uint64_t *C1, const spin_tuple *t1, const uint64_t *C2, const spin_tuple *t2,
                                 const uint64_t *row_words, const uint64_t *column_words, uint64_t *dx, uint64_t *dgamma, uint64_t *dbeta,
@@ -540,8 +540,7 @@ spin_status spin32_linattn_step(const spin_linattn *s, int rows, int columns, co
 spin_status spin32_layernorm(const spin_norm *s, int iterations, uint32_t offset, uint32_t slope, uint32_t eps, const uint32_t *x,
                            const spin_masked *gamma, const uint32_t *beta, const uint32_t *mask_x, const uint32_t *mask_xhat,
                            const uint32_t *C1, const spin_tuple *t1, const uint32_t *C2, const spin_tuple *t2, const uint32_t *row_words,
-                           uint32_t *out, uint32_t *xhat, uint32_t *rstd, void *workspace, size_t workspace_bytes, spin_stream stream);
-size_t spin32_layernorm_workspace_bytes(const spin_norm *s);
+                           uint32_t *out, uint32_t *xhat, uint32_t *rstd, spin_stream stream);
 spin_status spin32_layernorm_grad(const spin_norm *s, const spin_masked *dy, const spin_masked *xhat, const uint32_t *rstd, const spin_masked *gamma,
                                 const uint32_t *mask_g, const uint32_t *C1, const spin_tuple *t1, const uint32_t *C2, const spin_tuple *t2,
                                 const uint32_t *row_words, const uint32_t *column_words, uint32_t *dx, uint32_t *dgamma, uint32_t *dbeta,

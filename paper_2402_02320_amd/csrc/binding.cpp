@@ -43,7 +43,6 @@ template <> struct ByWord<uint64_t> {
     decltype(&spin_linattn_outputs) linattn_outputs;
     decltype(&spin_linattn_step) linattn_step;
     decltype(&spin_layernorm) norm;
-    decltype(&spin_layernorm_workspace_bytes) norm_bytes;
     decltype(&spin_layernorm_grad) norm_grad;
     decltype(&spin_layernorm_grad_workspace_bytes) norm_grad_bytes;
 };
@@ -64,7 +63,6 @@ template <> struct ByWord<uint32_t> {
     decltype(&spin32_linattn_outputs) linattn_outputs;
     decltype(&spin32_linattn_step) linattn_step;
     decltype(&spin32_layernorm) norm;
-    decltype(&spin32_layernorm_workspace_bytes) norm_bytes;
     decltype(&spin32_layernorm_grad) norm_grad;
     decltype(&spin32_layernorm_grad_workspace_bytes) norm_grad_bytes;
 };
@@ -813,7 +811,7 @@ template <class T> inline bool norm_of(const at::Tensor *x, PyObject *f, PyObjec
     s.n = (int)x->size(0), s.rows = (int)x->size(1), s.dim = (int)x->size(2);
     return true;
 }
-template <class T> PyObject *layernorm(PyObject *const *a)         // x, gamma, beta, masks, C, tuples, row_words, f, shift, line, eps, out, workspace
+template <class T> PyObject *layernorm(PyObject *const *a)         // x, gamma, beta, masks, C, tuples, row_words, f, shift, line, eps, out
 {
     const Operands<T> ops;
     const at::Tensor *x = word_tensor<T>(a[0]), *w = word_tensor<T>(a[6]);
@@ -829,7 +827,6 @@ template <class T> PyObject *layernorm(PyObject *const *a)         // x, gamma, 
     spin_tuple t[2];
     const T *value, *beta, *mask[2], *C[2], *row_words;
     Result<T> out, xhat, rstd;
-    Workspace ws;
     // xhat and rstd may be left out
     const bool keeps_xhat = a[11] == Py_None || PySequence_Fast_GET_ITEM(a[11], 1) != Py_None, keeps_rstd = a[11] == Py_None || PySequence_Fast_GET_ITEM(a[11], 2) != Py_None;
     if (!ops.word(a[0], s, value) || !ops.masked(a[1], Shape(columns, 2), gamma) || !ops.word(a[2], Shape(columns, 2), beta) || !ops.word(a[6], Shape(words, 3), row_words))
@@ -839,13 +836,13 @@ template <class T> PyObject *layernorm(PyObject *const *a)         // x, gamma, 
             !ops.tuple(PySequence_Fast_GET_ITEM(a[5], k), s, t[k]))
             return none();
     if (!ops.result(item(a[11], 0), s, *x, out) || (keeps_xhat && !ops.result(item(a[11], 1), s, *x, xhat)) ||
-        (keeps_rstd && !ops.result(item(a[11], 2), Shape(rows, 2), *x, rstd)) || !ws.take(a[12], by_word<T>().norm_bytes(&d), *x))
+        (keeps_rstd && !ops.result(item(a[11], 2), Shape(rows, 2), *x, rstd)))
         return none();
     T *to = data<T>(out.t), *to_xhat = keeps_xhat ? data<T>(xhat.t) : nullptr, *to_rstd = keeps_rstd ? data<T>(rstd.t) : nullptr;
     const int iterations = (int)(w->size(1) / 15) - 1;
     return run_all({out.t, xhat.t, rstd.t}, [&](spin_stream q) {
         return by_word<T>().norm(&d, iterations, (T)offset, (T)slope, (T)eps, value, &gamma, beta, mask[0], mask[1], C[0], &t[0], C[1], &t[1], row_words, to, to_xhat, to_rstd,
-                                 ws.space(), ws.bytes(), q);
+                                 q);
     });
 }
 template <class T> PyObject *layernorm_grad(PyObject *const *a)    // dy, xhat, rstd, gamma, masks, C, tuples, row_words, column_words, f, shift, out, workspace
@@ -927,7 +924,7 @@ PyMethodDef methods[] = {{"bind", (PyCFunction)(void *)bind, METH_FASTCALL, null
                          FAST("linattn_states", either(a, count, 13, linattn_states<uint64_t>, linattn_states<uint32_t>)),
                          FAST("linattn_outputs", either(a, count, 13, linattn_outputs<uint64_t>, linattn_outputs<uint32_t>)),
                          FAST("linattn_step", either(a, count, 12, linattn_step<uint64_t>, linattn_step<uint32_t>)),
-                         FAST("layernorm", either(a, count, 13, layernorm<uint64_t>, layernorm<uint32_t>)),
+                         FAST("layernorm", either(a, count, 12, layernorm<uint64_t>, layernorm<uint32_t>)),
                          FAST("layernorm_grad", either(a, count, 13, layernorm_grad<uint64_t>, layernorm_grad<uint32_t>)),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

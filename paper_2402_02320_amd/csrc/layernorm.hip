@@ -146,8 +146,6 @@ __global__ __launch_bounds__(kNormBlock<WAVES>, WAVES > 4 ? 4 : 1) void norm_ker
 
 }  // namespace
 
-size_t layernorm_workspace(int, int, int, int) { return 256; }
-
 template <class T> spin_status launch_layernorm(const NormArgs<T> &a, hipStream_t s)
 {
     KernelTimer timer(SPIN_KERNEL_LAYERNORM, s);

@@ -60,7 +60,6 @@ template <class T> struct NormArgs {
     Masked<T> gamma;
     Tuple<T> t1, t2;
     T *out, *xhat, *rstd;
-    void *workspace;
 };
 template <class T> struct NormGradArgs {
     int n, rows, dim, f, shift;
@@ -79,7 +78,6 @@ template <class T> spin_status launch_linattn_outputs(const OutputsArgs<T> &a, h
 template <class T> spin_status launch_linattn_step(const StepArgs<T> &a, hipStream_t s);
 template <class T> spin_status launch_layernorm(const NormArgs<T> &a, hipStream_t s);
 template <class T> spin_status launch_layernorm_grad(const NormGradArgs<T> &a, hipStream_t s);
-size_t layernorm_workspace(int n, int rows, int dim, int word_bytes);
 size_t layernorm_grad_workspace(int n, int rows, int dim, int word_bytes);
 
 constexpr int kNormWords = 15, kNormGradWords = 22;        // of a row: a Newton step's (and as many besides), the gradient's

@@ -112,11 +112,6 @@ spin_status check_norm(const spin_norm *s, int most)
 
 template <class T> T inverse(const spin_norm &s) { return (T)((((uint64_t)1 << s.shift) + s.dim / 2) / s.dim); }
 
-size_t norm_workspace(const spin_norm *s, int word_bytes)
-{
-    return check_norm(s, 8 * word_bytes - 3) == SPIN_OK ? layernorm_workspace(s->n, s->rows, s->dim, word_bytes) : 0;
-}
-
 size_t norm_grad_workspace(const spin_norm *s, int word_bytes)
 {
     return check_norm(s, 8 * word_bytes - 3) == SPIN_OK ? layernorm_grad_workspace(s->n, s->rows, s->dim, word_bytes) : 0;
@@ -124,17 +119,15 @@ size_t norm_grad_workspace(const spin_norm *s, int word_bytes)
 
 template <class T>
 spin_status run_norm(const spin_norm *s, int iterations, T offset, T slope, T eps, const T *x, const spin_masked *gamma, const T *beta, const T *mask_x, const T *mask_xhat,
-                 const T *C1, const spin_tuple *t1, const T *C2, const spin_tuple *t2, const T *row_words, T *out, T *xhat, T *rstd, void *workspace,
-                 size_t workspace_bytes, spin_stream stream)
+                 const T *C1, const spin_tuple *t1, const T *C2, const spin_tuple *t2, const T *row_words, T *out, T *xhat, T *rstd, spin_stream stream)
 {
     const spin_status st = check_norm(s, most_bits<T>);
     if (st != SPIN_OK) return st;
     if (iterations < 0 || iterations > SPIN_MAX_NORM_ITERATIONS || bad_ptr(x) || bad(gamma) || bad_ptr(beta) || bad_ptr(mask_x) || bad_ptr(mask_xhat) || bad_ptr(C1) ||
         bad(t1) || bad_ptr(C2) || bad(t2) || bad_ptr(row_words) || bad_ptr(out) || (xhat && bad_ptr(xhat)) || (rstd && bad_ptr(rstd)))
         return SPIN_EINVAL;
-    if (bad_workspace(workspace, workspace_bytes, layernorm_workspace(s->n, s->rows, s->dim, sizeof(T)))) return SPIN_EWORKSPACE;
     return launch_layernorm<T>({s->n, s->rows, s->dim, s->f, s->shift, iterations, inverse<T>(*s), offset, slope, eps, x, beta, C1, C2, row_words, mask_x, mask_xhat,
-                                of<T>(gamma), of<T>(t1), of<T>(t2), out, xhat, rstd, workspace}, (hipStream_t)stream);
+                                of<T>(gamma), of<T>(t1), of<T>(t2), out, xhat, rstd}, (hipStream_t)stream);
 }
 
 template <class T>
@@ -189,16 +182,9 @@ spin_status spin_linattn_step(const spin_linattn *s, int rows, int columns, cons
 
 spin_status spin_layernorm(const spin_norm *s, int iterations, uint64_t offset, uint64_t slope, uint64_t eps, const uint64_t *x, const spin_masked *gamma,
                            const uint64_t *beta, const uint64_t *mask_x, const uint64_t *mask_xhat, const uint64_t *C1, const spin_tuple *t1, const uint64_t *C2,
-                           const spin_tuple *t2, const uint64_t *row_words, uint64_t *out, uint64_t *xhat, uint64_t *rstd, void *workspace, size_t workspace_bytes,
-                           spin_stream stream)
+                           const spin_tuple *t2, const uint64_t *row_words, uint64_t *out, uint64_t *xhat, uint64_t *rstd, spin_stream stream)
 {
-    return run_norm<uint64_t>(s, iterations, offset, slope, eps, x, gamma, beta, mask_x, mask_xhat, C1, t1, C2, t2, row_words, out, xhat, rstd, workspace,
-                          workspace_bytes, stream);
-}
-
-size_t spin_layernorm_workspace_bytes(const spin_norm *s)
-{
-    return norm_workspace(s, sizeof(uint64_t));
+    return run_norm<uint64_t>(s, iterations, offset, slope, eps, x, gamma, beta, mask_x, mask_xhat, C1, t1, C2, t2, row_words, out, xhat, rstd, stream);
 }
 
 spin_status spin_layernorm_grad(const spin_norm *s, const spin_masked *dy, const spin_masked *xhat, const uint64_t *rstd, const spin_masked *gamma,
@@ -247,16 +233,9 @@ spin_status spin32_linattn_step(const spin_linattn *s, int rows, int columns, co
 
 spin_status spin32_layernorm(const spin_norm *s, int iterations, uint32_t offset, uint32_t slope, uint32_t eps, const uint32_t *x, const spin_masked *gamma,
                              const uint32_t *beta, const uint32_t *mask_x, const uint32_t *mask_xhat, const uint32_t *C1, const spin_tuple *t1, const uint32_t *C2,
-                             const spin_tuple *t2, const uint32_t *row_words, uint32_t *out, uint32_t *xhat, uint32_t *rstd, void *workspace, size_t workspace_bytes,
-                             spin_stream stream)
+                             const spin_tuple *t2, const uint32_t *row_words, uint32_t *out, uint32_t *xhat, uint32_t *rstd, spin_stream stream)
 {
-    return run_norm<uint32_t>(s, iterations, offset, slope, eps, x, gamma, beta, mask_x, mask_xhat, C1, t1, C2, t2, row_words, out, xhat, rstd, workspace,
-                          workspace_bytes, stream);
-}
-
-size_t spin32_layernorm_workspace_bytes(const spin_norm *s)
-{
-    return norm_workspace(s, sizeof(uint32_t));
+    return run_norm<uint32_t>(s, iterations, offset, slope, eps, x, gamma, beta, mask_x, mask_xhat, C1, t1, C2, t2, row_words, out, xhat, rstd, stream);
 }
 
 spin_status spin32_layernorm_grad(const spin_norm *s, const spin_masked *dy, const spin_masked *xhat, const uint32_t *rstd, const spin_masked *gamma,

@@ -113,8 +113,8 @@ def lib():
                 getattr(L, pre + name).restype = sz if name.endswith("_bytes") else i32
             for name, argtypes in (("linattn_scores", [p, i32] + [p] * 6), ("linattn_states", [p] + [i32] * 3 + [p] * 8 + [sz, p]),
                                    ("linattn_states_workspace_bytes", [p, i32, i32]), ("linattn_outputs", [p] + [i32] * 4 + [p] * 8),
-                                   ("linattn_step", [p, i32, i32] + [p] * 12), ("layernorm", [p, i32] + [word] * 3 + [p] * 14 + [sz, p]),
-                                   ("layernorm_grad", [p] * 16 + [sz, p]), ("layernorm_workspace_bytes", [p]), ("layernorm_grad_workspace_bytes", [p])):
+                                   ("linattn_step", [p, i32, i32] + [p] * 12), ("layernorm", [p, i32] + [word] * 3 + [p] * 14),
+                                   ("layernorm_grad", [p] * 16 + [sz, p]), ("layernorm_grad_workspace_bytes", [p])):
                 getattr(L, pre + name).argtypes = argtypes
                 getattr(L, pre + name).restype = sz if name.endswith("_bytes") else i32
         L.spin_probe_mfma.argtypes = [p, i32, i32, p, p]
@@ -143,7 +143,7 @@ def _load_binding(L):
     entries = ["spin_" + e for e in entries] + [pre + e for pre in ("spin_", "spin32_") for e in
                                                 ("cache_append", "cache_copy", "cache_compact", "cache_scores", "cache_values", "cache_values_workspace_bytes",
                                                  "relbias_trunc", "relbias_grad", "linattn_scores", "linattn_states", "linattn_states_workspace_bytes", "linattn_outputs",
-                                                 "linattn_step", "layernorm", "layernorm_workspace_bytes", "layernorm_grad", "layernorm_grad_workspace_bytes")]
+                                                 "linattn_step", "layernorm", "layernorm_grad", "layernorm_grad_workspace_bytes")]
     binding.bind(tuple(ctypes.cast(getattr(L, e), ctypes.c_void_p).value for e in entries), _UNASKED_BYTES)
     _fast = binding
 
@@ -1065,41 +1065,28 @@ class _Word:
         _shapes(x.dim() == 3)
         return _Norm(*_ints(*x.shape, f, shift))
 
-    def _norm_workspace(self, name, s, workspace, device):
-        if workspace is None:
-            size = int(self.entry(name + "_workspace_bytes")(ctypes.byref(s)))
-            if size == 0:
-                raise SpinError("invalid dimensions of a layer norm")
-            workspace = torch.empty(size, dtype=torch.uint8, device=device)
-        _on_this_device(workspace, "workspace")
-        return workspace, _workspace_ptr(workspace), workspace.numel() * workspace.element_size()
-
-    def layernorm_workspace_bytes(self, n, rows, dim):
-        return int(self.entry("layernorm_workspace_bytes")(ctypes.byref(_Norm(*_ints(n, rows, dim, 1, 1)))))
-
     def layernorm_grad_workspace_bytes(self, n, rows, dim):
         return int(self.entry("layernorm_grad_workspace_bytes")(ctypes.byref(_Norm(*_ints(n, rows, dim, 1, 1)))))
 
-    def layernorm(self, x, gamma, beta, masks, C, tuples, row_words, f, shift, line, eps=0, out=None, workspace=None):
+    def layernorm(self, x, gamma, beta, masks, C, tuples, row_words, f, shift, line, eps=0, out=None):
         """Layer norm of rows x [n, rows, dim]: (result, xhat, rstd).  gamma: (shares, masks), [n, dim], as beta; masks, C, tuples: two each, of the centred rows and of
         xhat, all as x; row_words: [n, 15 (iterations + 1), rows], in the order listed at spin_layernorm.  Means are sums times round(2^shift / dim), truncated by shift;
         1 / sqrt(variance + eps) is Newton's from the public line (offset, slope), offset - slope * variance; eps, offset, slope: words at f bits."""
         if _fast is not None:
-            done = _fast.layernorm(self.bits, x, gamma, beta, masks, C, tuples, row_words, f, shift, line, eps, out, workspace)
+            done = _fast.layernorm(self.bits, x, gamma, beta, masks, C, tuples, row_words, f, shift, line, eps, out)
             if done is not None:
                 return _done(done)
         s = self._norm(x, f, shift)
         n, rows, dim = shape = tuple(x.shape)
         _shapes(row_words.dim() == 3 and row_words.shape[1] % 15 == 0 and row_words.shape[1] > 0)
         result, xhat, rstd = (torch.empty_like(x), torch.empty_like(x), x.new_empty((n, rows))) if out is None else out
-        workspace, at, size = self._norm_workspace("layernorm", s, workspace, x.device)
         offset, slope = line
         _check(self.entry("layernorm")(ctypes.byref(s), row_words.shape[1] // 15 - 1, *[v % (1 << self.bits) for v in (offset, slope, eps)], self._of(x, "x"),
                                        self._masked(gamma, "gamma", n, dim), self._of(beta, "beta", n, dim), self._of(masks[0], "mask", *shape),
                                        self._of(masks[1], "mask", *shape), self._of(C[0], "C", *shape), self._tuple(tuples[0], *shape), self._of(C[1], "C", *shape),
                                        self._tuple(tuples[1], *shape), self._of(row_words, "row_words", n, row_words.shape[1], rows),
                                        self._to(result, "out", x.numel()), None if xhat is None else self._to(xhat, "xhat", x.numel()),
-                                       None if rstd is None else self._to(rstd, "rstd", n * rows), at, size, _stream()))
+                                       None if rstd is None else self._to(rstd, "rstd", n * rows), _stream()))
         return result, xhat, rstd
 
     def layernorm_grad(self, dy, xhat, rstd, gamma, masks, C, tuples, row_words, column_words, f, shift, out=None, workspace=None):
@@ -1112,18 +1099,24 @@ class _Word:
         s = self._norm(dy, f, shift)
         n, rows, dim = shape = tuple(dy.shape)
         dx, dgamma, dbeta = (torch.empty_like(dy), dy.new_empty((n, dim)), dy.new_empty((n, dim))) if out is None else out
-        workspace, at, size = self._norm_workspace("layernorm_grad", s, workspace, dy.device)
+        if workspace is None:
+            size = int(self.entry("layernorm_grad_workspace_bytes")(ctypes.byref(s)))
+            if size == 0:
+                raise SpinError("invalid dimensions of a layer norm")
+            workspace = torch.empty(size, dtype=torch.uint8, device=dy.device)
+        _on_this_device(workspace, "workspace")
         _check(self.entry("layernorm_grad")(ctypes.byref(s), self._masked((dy, masks[0]), "dy", *shape), self._masked((xhat, masks[1]), "xhat", *shape),
                                             self._of(rstd, "rstd", n, rows), self._masked(gamma, "gamma", n, dim), self._of(masks[2], "mask", *shape),
                                             self._of(C[0], "C", *shape), self._tuple(tuples[0], *shape), self._of(C[1], "C", *shape), self._tuple(tuples[1], *shape),
                                             self._of(row_words, "row_words", n, 22, rows), self._of(column_words, "column_words", n, 4, dim),
-                                            self._to(dx, "out", dy.numel()), self._to(dgamma, "out", n * dim), self._to(dbeta, "out", n * dim), at, size, _stream()))
+                                            self._to(dx, "out", dy.numel()), self._to(dgamma, "out", n * dim), self._to(dbeta, "out", n * dim),
+                                            _workspace_ptr(workspace), workspace.numel() * workspace.element_size(), _stream()))
         return dx, dgamma, dbeta
 
 
 _CALLS_BY_WORD = ("cache_append", "cache_copy", "cache_compact", "cache_scores", "cache_values", "cache_values_workspace_bytes", "relbias_trunc", "relbias_grad",
                   "linattn_scores", "linattn_states", "linattn_states_workspace_bytes", "linattn_outputs", "linattn_step",
-                  "layernorm", "layernorm_workspace_bytes", "layernorm_grad", "layernorm_grad_workspace_bytes")
+                  "layernorm", "layernorm_grad", "layernorm_grad_workspace_bytes")
 for _name in _CALLS_BY_WORD:
     globals()[_name] = getattr(_Word(64), _name)
     setattr(ring32, _name, staticmethod(getattr(_Word(32), _name)))

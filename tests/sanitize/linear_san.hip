@@ -25,7 +25,6 @@ namespace spin {
     template <> spin_status launch_layernorm_grad<T>(const NormGradArgs<T> &a, hipStream_t) { return inverse_seen = a.inv, ++launched, SPIN_OK; }
 NOTED(u64)
 NOTED(u32)
-size_t layernorm_workspace(int, int, int, int) { return 256; }
 size_t layernorm_grad_workspace(int, int, int, int) { return 256; }
 }  // namespace spin
 
@@ -72,14 +71,14 @@ int main()
             int *const at[] = {&s.n, &s.rows, &s.dim, &s.f, &s.shift};
             *at[field] = v;
             const int before = launched;
-            const spin_status st = spin32_layernorm(&s, 2, 1, 1, 1, q, &m, q, q, q, q, &t, q, &t, q, q, nullptr, nullptr, q, 256, nullptr);
+            const spin_status st = spin32_layernorm(&s, 2, 1, 1, 1, q, &m, q, q, q, q, &t, q, &t, q, q, nullptr, nullptr, nullptr);
             CHECK(st == spin32_layernorm_grad(&s, &m, &m, q, &m, q, q, &t, q, &t, q, q, q, q, q, q, 256, nullptr));
             CHECK(launched - before == (st == SPIN_OK ? 2 : 0));
-            CHECK((spin32_layernorm_workspace_bytes(&s) != 0) == (st == SPIN_OK));
+            CHECK((spin32_layernorm_grad_workspace_bytes(&s) != 0) == (st == SPIN_OK));
             if (st == SPIN_OK) CHECK(inverse_seen == (((u64)1 << s.shift) + s.dim / 2) / s.dim);
         }
     spin_norm wide{8, 1, 1, 60, 61};
-    CHECK(spin_layernorm(&wide, 16, 1, 1, 1, p, &m, p, p, p, p, &t, p, &t, p, p, p, p, p, 256, nullptr) == SPIN_OK && inverse_seen == (u64)1 << 61);
+    CHECK(spin_layernorm(&wide, 16, 1, 1, 1, p, &m, p, p, p, p, &t, p, &t, p, p, p, p, nullptr) == SPIN_OK && inverse_seen == (u64)1 << 61);
     printf("run ok\n");
     return 0;
 }
