@@ -55,7 +55,7 @@ template <int TILE> constexpr int kProductBlock = 8 * TILE;
 template <class T, int TILE> constexpr int kSlot = TILE / 32 * (int)sizeof(T) * kFrag;             // one factor's digits of TILE x 32
 template <int NP, class T, int TILE> constexpr int kGroup = TILE == 32 || NP < 3 ? NP : 3;
 enum Weight { kNone, kByRow, kByK };
-template <int NP, class T, int TILE, Weight W> constexpr int kAhead = TILE == 32 || NP == 1 || NP > kGroup<NP, T, TILE> || (NP == 3 && W != kNone) ? 1 : 2;
+template <int NP, class T, int TILE, Weight W> constexpr int kAhead = NP == 1 || NP > 3 || (TILE == 32 && sizeof(T) == 4) || (NP == 3 && (TILE == 64 ? W != kNone : W == kByRow)) ? 1 : 2;
 template <int NP, class T, int TILE> constexpr int product_lds = 2 * (kGroup<NP, T, TILE> + 1) * kSlot<T, TILE>;
 template <int NP, class T, int TILE> constexpr int kProductOccupancy = sizeof(T) == 4 && NP > 1 ? 4 : 2;          // waves a SIMD
 
@@ -108,7 +108,8 @@ template <class T> __device__ inline void digits_of(const T *w, u32 (&d)[sizeof(
 __device__ inline int place(int row, int half) { return (half * 32 + row % 2 * 16 + (row / 2 + row % 2 * 8 + half * 4) % 16) * 16; }
 
 // The sums of a tile over two ranges of k, in LDS as words when it returns (all waves have passed a barrier): sum_at().
-template <int NP, class T, int TILE, Weight WEIGH> __device__ inline void product_tile(const Segment<T> &one, const Segment<T> &two, char *lds)
+// `then` is called before they meet, when every wave's digits are words and their registers free: what it loads is under way meanwhile.
+template <int NP, class T, int TILE, Weight WEIGH, class Then> __device__ inline void product_tile(const Segment<T> &one, const Segment<T> &two, char *lds, Then &&then)
 {
     constexpr int ND = sizeof(T), GROUP = kGroup<NP, T, TILE>, WAVES = TILE / 8, SIDE = 4 * TILE, HALF = TILE / 2, kBlock = ND * kFrag;
     constexpr int kPitch = TILE + 1;
@@ -185,11 +186,16 @@ template <int NP, class T, int TILE, Weight WEIGH> __device__ inline void produc
             }
         }
     };
+    // The upper four digits' sums only have 32 bits to give.
     auto word = [&](int r) __attribute__((always_inline)) {
-        T v = 0;
+        u32 high = 0;
 #pragma unroll
-        for (int d = ND - 1; d >= 0; --d) v = (v << 8) + (T)(std::make_signed_t<T>)acc[d][r];
-        return v;
+        for (int d = ND - 4; d < ND; ++d) high += (u32)acc[d][r] << (8 * (d - ND + 4));
+        if constexpr (ND == 4) return (T)high;
+        int64_t v = acc[0][r];
+#pragma unroll
+        for (int d = 1; d < 4; ++d) v += (int64_t)acc[d][r] * (1 << (8 * d));
+        return (T)v + ((T)high << (8 * sizeof(T) - 32));
     };
     auto load_party = [&](int to, int t, int i) __attribute__((always_inline)) {
         const bool second = t >= steps0;
@@ -224,6 +230,13 @@ template <int NP, class T, int TILE, Weight WEIGH> __device__ inline void produc
                 w[e] = k < g.end && k <= row + g.below && k >= row + g.above ? w[e] : 0;
             }
         };
+        // Weights by k are asked for before the parties' words are dealt with, where those leave registers.
+        constexpr bool EARLY = WEIGH == kByK && AHEAD == 1;
+        T by_k[EARLY ? 4 : 1];
+        auto weight_of = [&](int e) __attribute__((always_inline)) { return g.w ? g.w[min(k0 + k_of(s.along, e), s.ks - 1) * g.stride] : 1; };
+        if (EARLY)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) by_k[EARLY ? e : 0] = weight_of(e);
         pair open[4];
 #pragma unroll
         for (int v = 0; v < 4; ++v) open[v] = pair{0, 0};
@@ -267,7 +280,7 @@ template <int NP, class T, int TILE, Weight WEIGH> __device__ inline void produc
             for (int e = 0; e < 4; ++e) w[e] = word_of(open, s.along, half, e);
             if (WEIGH == kByK && g.w)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) w[e] *= g.w[min(k0 + k_of(s.along, e), s.ks - 1) * g.stride];
+                for (int e = 0; e < 4; ++e) w[e] *= EARLY ? by_k[EARLY ? e : 0] : weight_of(e);
             weigh(w, half);
             stage(w, half, 0, s.along);
         }
@@ -296,19 +309,27 @@ template <int NP, class T, int TILE, Weight WEIGH> __device__ inline void produc
         }
     }
     // The waves' sums meet in LDS: of tiles of 64 those of one product in front of the other's, of tiles of 32 one product's in a part of its own.
+    T sums[16];
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+        sums[r] = word(r);
+        computed_here(sums[r]);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    then();
+    __builtin_amdgcn_sched_barrier(0);
     __syncthreads();
     constexpr int PARTS = TILE == 64 ? 1 : 2;
     T *const to = (T *)lds + (right ? (PARTS - 1) * TILE * kPitch + (wm * 32 + lane % 32) * kPitch + wn * 32 + 4 * (lane / 32)
                                     : (wm * 32 + 4 * (lane / 32)) * kPitch + wn * 32 + lane % 32);
     const int stride = right ? 1 : kPitch, turn = TILE == 64 ? (right ? 1 : 0) : wave % 2;
-#pragma unroll 1
+#pragma unroll
     for (int half = 0; half < 2; ++half) {
         if (turn == half) {
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
                 T &sum = to[(8 * (r / 4) + r % 4) * stride];
-                sum = (half ? sum : 0) + word(r);
-                if (r % 4 == 3) __builtin_amdgcn_sched_barrier(0);
+                sum = (half ? sum : 0) + sums[r];
             }
         }
         __syncthreads();
@@ -410,9 +431,8 @@ template <int NP, class T, int TILE> __global__ __launch_bounds__(kProductBlock<
     const Segment<T> s{{a.x.x + (token + i0) * a.dim, a.x.a + (token + i0) * a.dim, party, (u32)a.dim, true, u.L - i0, a.dim},
                        {a.y.x + (token + j0) * a.dim, a.y.a + (token + j0) * a.dim, party, (u32)a.dim, true, u.L - j0, a.dim},
                        {0, a.dim, kEverywhere, -kEverywhere, nullptr, 0, 0}};
-    product_tile<NP, T, TILE, kNone>(s, nothing_after(s), lds);
     Rows<NP, T, TILE, true> rows{a.C, a.t, each, first + (size_t)i0 * C + j0, (u32)C, min(u.L, C) - i0, C - j0, i0 - j0};
-    rows.load(0);
+    product_tile<NP, T, TILE, kNone>(s, nothing_after(s), lds, [&] { rows.load(0); });
     const int d = rows.column(), j = j0 + d;
 #pragma unroll 1
     for (int round = 0; round < rows.kRounds; ++round) {
@@ -447,9 +467,8 @@ template <int NP, class T, int TILE> __global__ __launch_bounds__(kProductBlock<
     const Segment<T> s{{a.x.x + token * a.rows + r0, a.x.a + token * a.rows + r0, heads * a.c.tokens * a.rows, (u32)a.rows, false, a.rows - r0, u.L},
                        {a.y.x + token * a.columns + d0, a.y.a + token * a.columns + d0, heads * a.c.tokens * a.columns, (u32)a.columns, false, a.columns - d0, u.L},
                        {0, u.L, kEverywhere, -kEverywhere, w, a.reverse ? 1 : -1, 0}};
-    product_tile<NP, T, TILE, kByK>(s, nothing_after(s), lds);
     Rows<NP, T, TILE, false> rows{a.C, a.t, each, at.unit * state + (size_t)r0 * a.columns + d0, (u32)a.columns, min(TILE, a.rows - r0), min(TILE, a.columns - d0), kEverywhere};
-    rows.load(0);
+    product_tile<NP, T, TILE, kByK>(s, nothing_after(s), lds, [&] { rows.load(0); });
 #pragma unroll 1
     for (int round = 0; round < rows.kRounds; ++round) {
 #pragma unroll
@@ -487,9 +506,8 @@ template <int NP, class T, int TILE> __global__ __launch_bounds__(kProductBlock<
                             {a.S.x + state, a.S.a + state, heads * a.c.chunks * a.rows * a.columns, (u32)(a.transposed ? a.rows : a.columns), a.transposed, a.columns - d0,
                              a.rows},
                             {0, a.rows, kEverywhere, -kEverywhere, w, a.reverse ? -1 : 1, 0}};
-    product_tile<NP, T, TILE, kByRow>(own, before, lds);
     Rows<NP, T, TILE, true> rows{a.C, a.t, each, (token + i0) * a.columns + d0, (u32)a.columns, min(u.L, there) - i0, min(TILE, a.columns - d0), kEverywhere};
-    rows.load(0);
+    product_tile<NP, T, TILE, kByRow>(own, before, lds, [&] { rows.load(0); });
     const int d = rows.column();
 #pragma unroll 1
     for (int round = 0; round < rows.kRounds; ++round) {
