@@ -55,7 +55,7 @@ template <int TILE> constexpr int kProductBlock = 8 * TILE;
 template <class T, int TILE> constexpr int kSlot = TILE / 32 * (int)sizeof(T) * kFrag;             // one factor's digits of TILE x 32
 template <int NP, class T, int TILE> constexpr int kGroup = TILE == 32 || NP < 3 ? NP : 3;
 enum Weight { kNone, kByRow, kByK };
-template <int NP, class T, int TILE, Weight W> constexpr int kAhead = NP == 1 || NP > 3 || (TILE == 32 && sizeof(T) == 4) || (NP == 3 && (TILE == 64 ? W != kNone : W == kByRow)) ? 1 : 2;
+template <int NP, class T, int TILE, Weight W> constexpr int kAhead = NP == 1 || NP > 3 || (TILE == 32 ? sizeof(T) == 4 : NP == 3 && W == kByK) ? 1 : 2;
 template <int NP, class T, int TILE> constexpr int product_lds = 2 * (kGroup<NP, T, TILE> + 1) * kSlot<T, TILE>;
 template <int NP, class T, int TILE> constexpr int kProductOccupancy = sizeof(T) == 4 && NP > 1 ? 4 : 2;          // waves a SIMD
 
@@ -116,7 +116,7 @@ template <int NP, class T, int TILE, Weight WEIGH, class Then> __device__ inline
     const u32 lane = threadIdx.x % 64;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     const bool right = wave >= WAVES / 2;
-    const u32 u = threadIdx.x % SIDE;  // among the threads of a side
+    u32 u = threadIdx.x % SIDE;        // among the threads of a side
     char *const rights = lds + (GROUP + 1) * kSlot<T, TILE>, *const mine = right ? rights : lds;
     const Side<T> side0 = either(right, one.left, one.right), side1 = either(right, two.left, two.right);
     auto steps = [](const Range<T> &k) { return k.end > k.begin ? (k.end - k.begin + kStep - 1) / kStep : 0; };
@@ -243,6 +243,7 @@ template <int NP, class T, int TILE, Weight WEIGH, class Then> __device__ inline
         __syncthreads();                                   // the last step's digits have been read
         // A party's words: its masks' digits, four words at a time.
         auto take = [&](const pair (&value)[4], const pair (&mask)[4], int i) __attribute__((always_inline)) {
+            if (AHEAD > 1) computed_here(u);  // places are made of it again: kept, they take registers that words need
 #pragma unroll
             for (int v = 0; v < 4; ++v) open[v] += value[v] - mask[v];
             if (i >= GROUP) return;
