@@ -163,10 +163,15 @@ template <int NP, class T, int TILE, Weight WEIGH, class Then> __device__ inline
     // Tiles of 32: the workgroups of a CU begin with different parties, so that where the parties are odd their SIMDs have the same work.  Four digits of the own factor at a time: all
     // eight take registers that the next words need.
     const int begin = TILE == 64 ? 1 : 1 + (wave + blockIdx.x / kXcds) % 2, by = TILE == 64 ? 1 : 2;
-    auto multiply = [&](int parties) __attribute__((always_inline)) {
+    auto multiply = [&](int parties, auto &&between) __attribute__((always_inline)) {
         asm volatile("" : "+s"(parties));                  // a loop for one party, too: unrolled, its products take a second set of sums
 #pragma unroll
         for (int d0 = 0; d0 < ND; d0 += 4) {
+            if (d0) {
+                __builtin_amdgcn_sched_barrier(0);
+                between();
+                __builtin_amdgcn_sched_barrier(0);
+            }
             v4i kept[4];
 #pragma unroll
             for (int d = 0; d < 4; ++d) kept[d] = *(const v4i *)(own + (d0 + d) * kFrag);
@@ -201,13 +206,15 @@ template <int NP, class T, int TILE, Weight WEIGH, class Then> __device__ inline
         const bool second = t >= steps0;
         load(either(second, side0, side1), second ? two.k.begin + (t - steps0) * kStep : one.k.begin + t * kStep, i, false, x[to], a[to]);
     };
-    // The words of AHEAD parties are under way, the next step's during the products.
-    auto load_ahead = [&](int t) __attribute__((always_inline)) {
+    // The words of AHEAD parties are under way, the next step's during the products: one party's asked for before the first half of the digits, one's before the second.  All at
+    // once, their requests wait for one another and the products for them.
+    constexpr int BETWEEN = AHEAD > 1 && ND > 4 ? 1 : 0;
+    auto load_ahead = [&](int t, int begin, int end) __attribute__((always_inline)) {
 #pragma unroll
-        for (int i = NP - 1; i >= NP - AHEAD; --i) load_party(i % AHEAD, t, i);
+        for (int i = NP - 1 - begin; i >= NP - end; --i) load_party(i % AHEAD, t, i);
     };
     __shared__ T by_row[TILE];
-    if (total) load_ahead(0);
+    if (total) load_ahead(0, 0, AHEAD);
 #pragma unroll 1
     for (int t = 0; t < total; ++t) {
         const bool second = t >= steps0;
@@ -286,11 +293,13 @@ template <int NP, class T, int TILE, Weight WEIGH, class Then> __device__ inline
             stage(w, half, 0, s.along);
         }
         __builtin_amdgcn_sched_barrier(0);
-        if (AHEAD > 1 && t + 1 < total) load_ahead(t + 1);
+        if (AHEAD > 1 && t + 1 < total) load_ahead(t + 1, 0, AHEAD - BETWEEN);
 #pragma unroll 1
         for (int first = 0;;) {
             __syncthreads();
-            multiply(min(GROUP, NP - first));
+            multiply(min(GROUP, NP - first), [&] {
+                if (BETWEEN && t + 1 < total) load_ahead(t + 1, AHEAD - BETWEEN, AHEAD);
+            });
             first += GROUP;
             if (first >= NP) break;
             __syncthreads();
