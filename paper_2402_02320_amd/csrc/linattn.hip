@@ -50,6 +50,10 @@ template <int NP, class T> __device__ inline void finish(T z, const T *C, const 
 // Tiles of 64: eight waves, of either product one has a 32 x 32 quarter; more parties than GROUP read the others' masks a second time.  Tiles of 32: four waves, of either product
 // one has every second party; for few chunks, where the larger ones leave CUs idle.
 // A factor is stored along its rows or along k; only the left one is cleared where it does not count, and weighed.
+//
+// Bound by the way of the factors' words to a CU and by what does not overlap with it: 3 parties, 32 heads of 128, 4096 tokens, chunks of 128: scores 0.67 ms (HBM's time for their
+// words 0.58), outputs 1.19, a chunk's part of the next state 0.60.  Of the 15,000 cycles of a step (2 parties, tiles of 64) the words' opening and splitting take 3,000, requests
+// for the next ones 4,700, the products 5,000: registers (128 of sums, 64 of words under way) and LDS (96 to 128 KB) let one workgroup of eight waves on a CU.
 constexpr int kStep = 32;              // k
 template <int TILE> constexpr int kProductBlock = 8 * TILE;
 template <class T, int TILE> constexpr int kSlot = TILE / 32 * (int)sizeof(T) * kFrag;             // one factor's digits of TILE x 32
@@ -535,7 +539,8 @@ template <int NP, class T, int TILE> __global__ __launch_bounds__(kProductBlock<
     }
 }
 
-// From chunk to chunk, a thread an element of the state: a stream of 3 NP + 1 words an element, those of kScanAtOnce chunks under way together.  Where a chunk has no tokens its
+// From chunk to chunk, a thread an element of the state: a stream of 3 NP + 1 words an element, those of kScanAtOnce chunks under way together: 3 parties, 32 heads of 128 x 128, 32
+// chunks 227 us, 5.9 TB/s.  Where a chunk has no tokens its
 // part of `opened` was not written: what is read of it is not used.
 template <int NP> constexpr int kScanAtOnce = NP <= 3 ? 4 : NP <= 6 ? 2 : 1;
 template <int NP, class T> __global__ __launch_bounds__(kBlock) void scan_kernel(StatesArgs<T> a)
@@ -582,7 +587,8 @@ template <int NP, class T> __global__ __launch_bounds__(kBlock) void scan_kernel
 
 // ---- a single token -----------------------------------------------------------------------------------------
 // A workgroup has `wide` columns of one head's state (a power of two), a thread one of them and every (kStepBlock / wide)-th row: all words of a state element are read and
-// written once, 7 a party, and what q . S' takes of them is added in registers, then in LDS.
+// written once, 7 a party, and what q . S' takes of them is added in registers, then in LDS.  Bound by HBM for many heads: 3 parties, 512 of 128 x 128, 254 us, 4.6 TB/s (a seventh
+// of it written); by a launch and two waits for memory for few: 16 of 64 x 64 8.6 us.
 constexpr int kStepBlock = 256;
 template <int NP, class T> __global__ __launch_bounds__(kStepBlock) void step_kernel(StepArgs<T> a, int wide, bool streamed)
 {
@@ -663,8 +669,8 @@ inline spin_status launch_products(Kernel kernel, const Args &a, int rows, int c
     return st;
 }
 // Tiles of 64 read and split every factor half as often, tiles of 32 are four times as many.  3 parties, 2 x 16 heads of 128, 4096 tokens in chunks of 128 (64-bit words): a prompt
-// 2.85 ms by 64, 3.24 by 32; 8 heads of 64, 300 tokens (40 tiles of 64): 102 us by 64, 66 by 32; 2 parties' training step of 16 heads of 64, 1024 tokens (256 tiles) 344
-// and 368.  32-bit words, which have fewer products to wait for: 24 heads of 80 and 48, chunks of 32, 125 us and 98.
+// 2.70 ms by 64, 2.99 by 32; 8 heads of 64, 300 tokens (40 tiles of 64): 98 us by 64, 55 by 32; 2 parties' training step of 16 heads of 64, 1024 tokens (256 tiles) 307
+// and 336.  32-bit words, which have fewer products to wait for: 24 heads of 80 and 48, chunks of 32, 94 us and 73.
 constexpr long kWantedTiles = 256;
 template <class T, class F> inline void for_tile(const ChunkView &c, int rows, int columns, F &&fn)
 {
@@ -726,8 +732,10 @@ template <class T> spin_status launch_linattn_step(const StepArgs<T> &a, hipStre
 {
     KernelTimer timer(SPIN_KERNEL_LINATTN, s);
     const bool streamed = (size_t)a.n * a.batch * a.heads * a.rows * a.columns * sizeof(T) >= kStreamingBytes;
+    // Full lines where the CUs have enough of them: 3 parties, 512 heads of 128, 254 us by 64, 270 by 16, 490 by 8; 16 heads of 64 21.7, 8.5 and 8.7; 2 parties over Z_2^32, 45 heads
+    // of 40 and 72, 9.4, 6.2 and 7.8.
     int wide = 64;
-    while (wide > 8 && (long)a.batch * a.heads * ((a.columns + wide - 1) / wide) < 1024) wide /= 2;
+    while (wide > 16 && (long)a.batch * a.heads * ((a.columns + wide - 1) / wide) < 1024) wide /= 2;
     for_party_count(a.n, [&](auto np) {
         step_kernel<decltype(np)::value, T><<<dim3((a.columns + wide - 1) / wide, a.batch * a.heads), kStepBlock, 0, s>>>(a, wide, streamed);
     });

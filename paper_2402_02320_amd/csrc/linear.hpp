@@ -82,7 +82,8 @@ size_t layernorm_grad_workspace(int n, int rows, int dim, int word_bytes);
 
 constexpr int kNormWords = 15, kNormGradWords = 22;        // of a row: a Newton step's (and as many besides), the gradient's
 constexpr int kMostDim = 8192;
-// Waves a row.  Few rows get more waves than they need where all CUs are busy: 3 parties, 2 rows of 1024, 14.3 us by four waves, 12.3 by 16.
+// Waves a row: as many as hold its words in registers, four words a thread.  The gradient of 1568 rows of 256, 5 parties: 52 us by one wave, 62 by four, 140 by 16; forward, 3
+// parties: 4096 rows of 1024 287 by four, 303 by 16.  Few rows get more waves than they need where all CUs are busy: 2 rows of 1024 14.3 by four, 12.2 by 16.
 constexpr int norm_waves(int rows, int dim) { return dim <= 256 ? 1 : dim <= 1024 && rows > 256 ? 4 : 16; }
 
 namespace {
