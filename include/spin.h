@@ -517,7 +517,8 @@ spin_status spin_layernorm(const spin_norm *s, int iterations, uint64_t offset, 
  *     dx = T(C2 + g rstd - xhat k2, f) - k1, t2
  * Column word 0, words 3, 12, 17 and C1, C2 (of g rstd - xhat k2) are the dealt shares of the masks' products.  dy, xhat, C1, C2, t1, t2, dx: [n][rows][dim]; gamma, dgamma,
  * dbeta: [n][dim]; rstd: [n][rows].  xhat's mask may be the forward pass's.  dx may alias C2 or an array of t2.  workspace: device scratch of
- * spin_layernorm_grad_workspace_bytes() bytes (0 if the arguments are invalid), 256-byte aligned.                                                  */
+ * spin_layernorm_grad_workspace_bytes() bytes (0 if the arguments are invalid), 256-byte aligned.  The size does not shrink as n or, for one dim, rows grow: that of the
+ * largest batch does for all.                                                                                                                       */
 spin_status spin_layernorm_grad(const spin_norm *s, const spin_masked *dy, const spin_masked *xhat, const uint64_t *rstd, const spin_masked *gamma,
                                 const uint64_t *mask_g, const uint64_t *C1, const spin_tuple *t1, const uint64_t *C2, const spin_tuple *t2,
                                 const uint64_t *row_words, const uint64_t *column_words, uint64_t *dx, uint64_t *dgamma, uint64_t *dbeta,

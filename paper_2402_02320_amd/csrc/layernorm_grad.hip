@@ -231,24 +231,14 @@ template <int NP, class T> __global__ __launch_bounds__(kJoinBlock) void join_ke
     for (int i = 0; i < NP; ++i) a.dgamma[(size_t)i * a.dim + d] = c.truncated(i, top[i], msb[i]);
 }
 
-// Rows of one wave or workgroup, and how many groups of rows have sums of their own: those of a workgroup.  As many as are on the chip at once: more groups only add sums to be
-// written and joined (16 waves: one workgroup a CU).
-struct Runs { int run, groups; };
-inline Runs runs_of(int rows, int dim)
-{
-    const int waves = norm_waves(rows, dim), at_once = waves == 1 ? 4 : 1, wanted = waves == 1 ? 1024 : waves == 4 ? 1024 : 256;
-    const int run = (int)(((long)rows + (long)wanted * at_once - 1) / ((long)wanted * at_once));
-    return {run, (int)(((long)rows + (long)run * at_once - 1) / ((long)run * at_once))};
-}
-
 }  // namespace
 
-size_t layernorm_grad_workspace(int n, int rows, int dim, int word_bytes) { return (size_t)runs_of(rows, dim).groups * (n + 1) * dim * word_bytes; }
+size_t layernorm_grad_workspace(int n, int rows, int dim, int word_bytes) { return (size_t)norm_most_groups(rows, dim) * (n + 1) * dim * word_bytes; }
 
 template <class T> spin_status launch_layernorm_grad(const NormGradArgs<T> &a, hipStream_t s)
 {
     KernelTimer timer(SPIN_KERNEL_LAYERNORM, s);
-    const Runs r = runs_of(a.rows, a.dim);
+    const NormRuns r = norm_runs(a.rows, a.dim);
     const bool streamed = (size_t)a.n * a.rows * a.dim * sizeof(T) >= kStreamingBytes;
     T *const sums = (T *)a.workspace;
     for_party_count(a.n, [&](auto np) {

@@ -86,6 +86,23 @@ constexpr int kMostDim = 8192;
 // parties: 4096 rows of 1024 287 by four, 303 by 16.  Few rows get more waves than they need where all CUs are busy: 2 rows of 1024 14.3 by four, 12.2 by 16.
 constexpr int norm_waves(int rows, int dim) { return dim <= 256 ? 1 : dim <= 1024 && rows > 256 ? 4 : 16; }
 
+// The gradient's rows: of one wave or workgroup (`run` successive ones), and how many groups of rows have sums of their own: those of a workgroup.  As many as are on the chip at
+// once: more groups only add sums to be written and joined (16 waves: one workgroup a CU).
+struct NormRuns { int run, groups; };
+constexpr int norm_rows_at_once(int rows, int dim) { return norm_waves(rows, dim) == 1 ? 4 : 1; }
+constexpr int norm_wanted_groups(int rows, int dim) { return norm_waves(rows, dim) == 16 ? 256 : 1024; }
+constexpr NormRuns norm_runs(int rows, int dim)
+{
+    const long at_once = norm_rows_at_once(rows, dim), wanted = norm_wanted_groups(rows, dim) * at_once, run = (rows + wanted - 1) / wanted;
+    return {(int)run, (int)((rows + run * at_once - 1) / (run * at_once))};
+}
+// At least as many groups, and never fewer for more rows: 1025 rows in runs of two have half the groups of 1024, and a workspace for the largest batch has to do for all.
+constexpr int norm_most_groups(int rows, int dim)
+{
+    const int at_once = norm_rows_at_once(rows, dim), all = (int)(((long)rows + at_once - 1) / at_once), wanted = norm_wanted_groups(rows, dim);
+    return all < wanted ? all : wanted;
+}
+
 namespace {
 
 // A word that is read once, by nobody else: what the dealer gave for one element.
