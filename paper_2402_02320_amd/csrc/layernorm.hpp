@@ -79,9 +79,9 @@ __device__ inline void make_new(u32 &column)
     asm volatile("" : "+v"(column));
 }
 
-template <class F> inline void for_dim(int rows, int dim, F &&fn)    // waves a row, words a thread
+template <class F> constexpr void for_dim(int rows, int dim, F &&fn)    // waves a row, words a thread
 {
-    const std::integral_constant<int, 4> four;
+    constexpr std::integral_constant<int, 4> four{};
     switch (norm_waves(rows, dim)) {
     case 1: fn(std::integral_constant<int, 1>(), four); break;
     case 4: fn(four, four); break;

@@ -1,20 +1,33 @@
-"""The rules that say how many waves a row of the norm has, against what the cases of tests/test_gpu_norm_rows.py are there
+"""The rules that say how many waves a row of the norm has, and how many rows a wave or workgroup of its gradient, against what the cases of tests/test_gpu_norm_rows.py are there
 for: another rule would take them out of the tests unseen.  Compiled for the host, nothing runs."""
 import os
 import subprocess
 
 import pytest
 
-from test_gpu_norm_rows import FOUR_WAVES
+from test_gpu_norm_rows import FOUR_WAVES, SEVERAL_ROWS
 
 SOURCE = """#include "layernorm_grad.hip"
 using namespace spin;
+constexpr int words(int rows, int dim)
+{
+    int each = 0;
+    for_dim(rows, dim, [&](auto, auto e) { each = decltype(e)::value; });
+    return each;
+}
 """
 
 
 def claims():
     for n, rows, dim, _ in FOUR_WAVES.values():
         yield "norm_waves(%d, %d) == 4" % (rows, dim)
+    for (n, rows, dim, _), (waves, each, run), lean in SEVERAL_ROWS.values():
+        yield "norm_waves(%d, %d) == %d && words(%d, %d) == %d" % (rows, dim, waves, rows, dim, each)
+        yield "norm_runs(%d, %d).run == %d" % (rows, dim, run)
+        # the last group has fewer rows than the others
+        yield "norm_runs({0}, {1}).groups * norm_runs({0}, {1}).run * norm_rows_at_once({0}, {1}) > {0}".format(rows, dim)
+        for word, own in zip(("u64", "u32"), lean):
+            yield "kLean<%d, %s, %d, %d> == %s" % (n, word, waves, each, str(own).lower())
 
 
 def compiled(tmp_path, lines, more=""):
