@@ -433,7 +433,8 @@ spin_status spin32_relbias_grad(int n, int batch, int heads, int Q, int K, int f
 /* ---- Linear attention with a decay, and layer norm ----------------------------------------------------
  * What a transformer block without softmax multiplies.  A secret x is opened once, E = sum_i (x_i - a_i) against the mask a dealt for it, and
  * every product with it takes the same E: beside the dealt share C_i of the masks' product party i adds E . b_i + a_i . F, and party 0 E . F.  T(z, f)
- * is the truncation of spin_trunc by f bits.  Entry points spin32_* take the same structures over arrays of uint32_t.                          */
+ * is the truncation of spin_trunc by f bits, and as there z has to be from -2^62 to 2^62 - 1 (spin32_*: -2^30 to 2^30 - 1): attention's scores, states and results
+ * have to stay below 2^(62 - 2f - g) (2^(30 - 2f - g): 64 at f = 9, g = 6).  Entry points spin32_* take the same structures over arrays of uint32_t.  */
 typedef struct { const void *value, *mask; } spin_masked;          /* shares and the masks that they are opened against, of one shape */
 typedef struct { const void *r, *r_top, *r_msb; } spin_tuple;      /* a truncation tuple, of the result's shape                       */
 
@@ -478,7 +479,7 @@ spin_status spin_linattn_outputs(const spin_linattn *s, int rows, int columns, i
                                  uint64_t *out, spin_stream stream);
 
 /* One token of every sequence b with active[b] > 0 (active NULL: all):   S' = T(CS + 2^f w[1] S + w[0] k (x) v, f + g),   out = T(CO + q . S', f),
- * S' being opened against S_mask.  Of the others S' = S and out = 0.  s->tokens and s->chunk are not looked at, s->lengths is `active`, and decay is [heads][2].
+ * S' being opened against S_mask; sum CS = w[0] (sum a_k) (x) (sum a_v), sum CO = (sum a_q) . (sum S_mask).  Of the others S' = S and out = 0.  s->tokens and s->chunk are not looked at, s->lengths is `active`, and decay is [heads][2].
  * q, k: [n][batch][heads][rows]; v, CO, tO, out: [n][batch][heads][columns]; S, S_mask, CS, tS, S_out: [n][batch][heads][rows][columns].  S_out may alias S, S_mask, CS or
  * an array of tS; out CO or an array of tO.                                                                                 */
 spin_status spin_linattn_step(const spin_linattn *s, int rows, int columns, const uint64_t *S, const spin_masked *q, const spin_masked *k,
@@ -486,7 +487,8 @@ spin_status spin_linattn_step(const spin_linattn *s, int rows, int columns, cons
                               const spin_tuple *tO, uint64_t *S_out, uint64_t *out, spin_stream stream);
 
 /* Layer norm of rows of `dim` words at f fractional bits.  Means are sums times inv = (2^shift + dim / 2) / dim, truncated by `shift`: the larger the
- * more exact, as long as a sum of dim words times inv stays in the ring.  dim: 1 to 8192.                                   */
+ * more exact, as long as a sum of dim words times inv stays where T is exact: means and variances below 2^(62 - f - shift) (2^(30 - f - shift)).  So do all sums of products, at 2f
+ * bits: a row's squares, its g xhat, a column's dy xhat have to stay below 2^(62 - 2f) (2^(30 - 2f): 4096 at f = 9).  dim: 1 to 8192.               */
 typedef struct {
     int n, rows, dim;
     int f;                   /* 1 to 60 (28)                                                                         */
