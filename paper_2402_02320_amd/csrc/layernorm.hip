@@ -1,5 +1,6 @@
-// Layer norm of shares (spin_layernorm).  A stream of 13 words an element and party with a wait in the middle: 3 parties, 4096 rows of 1024 286 us, 4.6 TB/s.  Few rows are bound by
-// the chain, some seventy dependent steps: 2 rows of 1024 12.2 us.
+// Layer norm of shares (spin_layernorm).  A stream of 13 words an element and party with the chain in the middle: 3 parties, 4096 rows of 1024 286 us, 4.6 TB/s, bound by trips to
+// memory one after another: a column's words of the first phase are waited for before the next column's are asked for, and of 64-bit words the last phase's come in several batches (below).
+// Few rows are bound by the chain, some seventy dependent steps: 2 rows of 1024 12.2 us.
 #include "layernorm.hpp"
 
 namespace spin {
@@ -54,6 +55,7 @@ __global__ __launch_bounds__(kNormBlock<WAVES>, WAVES > 4 ? 4 : 1) void norm_ker
         }
         if (NP * EACH > 12) __builtin_amdgcn_sched_barrier(0);
     }
+    // One load a turn, waited for before the next: one wave a row takes five turns for three parties and six steps.
     for (int k = t; k < count * NP; k += THREADS) words[k] = a.row_words[((size_t)(k % NP) * count + k / NP) * a.rows + row];
     s = wave_sum(s);
     if (t % 64 == 0) partial[slot][0][wave] = s;
@@ -110,7 +112,8 @@ __global__ __launch_bounds__(kNormBlock<WAVES>, WAVES > 4 ? 4 : 1) void norm_ker
             c.add(e * shared[slot][1 + i] + (KEEP ? mask[j][KEEP ? i : 0] : word(a.mask_x, i)) * fr);
             top[i] = dealt(a.t1.r_top, i), msb[i] = dealt(a.t1.r_msb, i);
         }
-        // Where a thread has registers for them all its words are asked for at once; otherwise the second truncation's behind the first's.
+        // Where a thread has registers for them all its words can be asked for at once; otherwise the second truncation's behind the first's.  As built, 32-bit words of two parties are (22
+        // in one batch); of 64-bit words, three parties, four words a thread, the last column's, while the first three wait six to twelve times each.
         auto first_part = [&]() __attribute__((always_inline)) {
 #pragma unroll
             for (int i = 0; i < NP; ++i) {

@@ -1,5 +1,6 @@
-// The gradients of layer norm on shares (spin_layernorm_grad).  A stream of 14 words an element and party with a wait in the middle: 3 parties, 2048 rows of 2048 308 us, 4.6 TB/s, of
-// which the sums' join is 6; 5 parties, 1568 rows of 256 52 us.
+// The gradients of layer norm on shares (spin_layernorm_grad).  A stream of 14 words an element and party with the chain in the middle: 3 parties, 2048 rows of 2048 308 us, 4.6 TB/s, of
+// which the sums' join is 6; 5 parties, 1568 rows of 256 52 us.  Bound by trips to memory one after another: as built a column of the former waits about twelve times before the sums
+// and four times behind them, with one workgroup a CU to go on meanwhile.
 #include "layernorm.hpp"
 
 namespace spin {

@@ -51,9 +51,10 @@ template <int NP, class T> __device__ inline void finish(T z, const T *C, const 
 // one has every second party; for few chunks, where the larger ones leave CUs idle.
 // A factor is stored along its rows or along k; only the left one is cleared where it does not count, and weighed.
 //
-// Bound by the way of the factors' words to a CU and by what does not overlap with it: 3 parties, 32 heads of 128, 4096 tokens, chunks of 128: scores 0.67 ms (HBM's time for their
-// words 0.58), outputs 1.19, a chunk's part of the next state 0.60.  Of the 15,000 cycles of a step (2 parties, tiles of 64) the words' opening and splitting take 3,000, requests
-// for the next ones 4,700, the products 5,000: registers (128 of sums, 64 of words under way) and LDS (96 to 128 KB) let one workgroup of eight waves on a CU.
+// Bound by the way of the factors' words to a CU and by what does not overlap with it: 3 parties, 2 x 16 heads of 128, 4096 and 2730 tokens, chunks of 128: scores 0.67 ms (their 2.4 GB
+// take HBM 0.39 at the 6.2 TB/s of streams that mostly read), outputs 1.19 (4.1 GB, 0.66), a chunk's part of the next state 0.60 (2.1 GB, 0.34).  Of the 15,000 cycles of a step
+// (2 parties, tiles of 64) the words' opening and splitting take 3,000, requests for the next ones 4,700, the products 5,000: registers (128 of sums, 64 of words under way) and LDS
+// (96 to 128 KB) let one workgroup of eight waves on a CU.
 constexpr int kStep = 32;              // k
 template <int TILE> constexpr int kProductBlock = 8 * TILE;
 template <class T, int TILE> constexpr int kSlot = TILE / 32 * (int)sizeof(T) * kFrag;             // one factor's digits of TILE x 32
@@ -457,6 +458,7 @@ template <int NP, class T, int TILE> __global__ __launch_bounds__(kProductBlock<
             T *const to = a.out + rows.corner + (size_t)r * C + d;
             const bool there = j <= i && i < u.L;
             Opened<T> c{a.c.f + a.c.g};
+            // The weight is asked for behind the dealt words and waited for with them, row by row: up to four trips to memory in a round.
             if (there) c.add(rows.masked(k, weight(a.decay, u.h, C, i - j) * sum_at<T, TILE>(lds, r, d)));
 #pragma unroll
             for (int p = 0; p < NP; ++p) to[p * each] = there ? c.truncated(p, rows.top[k][p], rows.msb[k][p]) : 0;
@@ -587,8 +589,9 @@ template <int NP, class T> __global__ __launch_bounds__(kBlock) void scan_kernel
 
 // ---- a single token -----------------------------------------------------------------------------------------
 // A workgroup has `wide` columns of one head's state (a power of two), a thread one of them and every (kStepBlock / wide)-th row: all words of a state element are read and
-// written once, 7 a party, and what q . S' takes of them is added in registers, then in LDS.  Bound by HBM for many heads: 3 parties, 512 of 128 x 128, 254 us, 4.6 TB/s (a seventh
-// of it written); by a launch and two waits for memory for few: 16 of 64 x 64 8.6 us.
+// written once, 7 a party, and what q . S' takes of them is added in registers, then in LDS.  Bound by trips to memory one after another: the factors', then a thread's rows' (no
+// load goes before the last row's stores, which may be to its words), a row's in two batches of three parties and six of five, since the first words are added before the last are
+// asked for.  3 parties: 16 heads of 64 x 64, four rows a thread, 8.5 us, 6.9 of them in the kernel; 512 of 128 x 128, 32 rows a thread, 254 us, 4.6 TB/s (a seventh of it written).
 constexpr int kStepBlock = 256;
 template <int NP, class T> __global__ __launch_bounds__(kStepBlock) void step_kernel(StepArgs<T> a, int wide, bool streamed)
 {
@@ -670,7 +673,14 @@ inline spin_status launch_products(Kernel kernel, const Args &a, int rows, int c
 }
 // Tiles of 64 read and split every factor half as often, tiles of 32 are four times as many.  3 parties, 2 x 16 heads of 128, 4096 tokens in chunks of 128 (64-bit words): a prompt
 // 2.70 ms by 64, 2.99 by 32; 8 heads of 64, 300 tokens (40 tiles of 64): 98 us by 64, 55 by 32; 2 parties' training step of 16 heads of 64, 1024 tokens (256 tiles) 307
-// and 336.  32-bit words, which have fewer products to wait for: 24 heads of 80 and 48, chunks of 32, 94 us and 73.
+// and 336.  By the number of tiles of 64, heads and chunks of 64, 3 parties, us of scores, states, outputs by 64 : by 32 (a tile of 64 takes a CU, so that the 257th begins a second
+// round):
+//     100    31 : 22     32 : 27     45 : 33            300    67 : 52     73 : 64    110 : 90            512    90 : 91    102 : 109   133 : 146
+//     200    37 : 37     43 : 46     57 : 64            400    78 : 74     88 : 90    115 : 120           600   116 : 107   129 : 126   175 : 168
+//     256    43 : 42     52 : 53     67 : 74            768   133 : 136   154 : 160   195 : 214          1024   176 : 178   202 : 210   265 : 277
+// 2 parties alike; 5, which read masks twice by 64 and wait for every party by 32: 100 51 : 45, 52 : 49, 86 : 82; 256 76 : 101, 85 : 110, 125 : 178; 300 122 : 119, 123 : 128, 199 : 216;
+// 1024 300 : 383, 331 : 414, 468 : 690.  So between one round and about 350 tiles the rule loses up to a quarter with few parties.
+// 32-bit words have tiles of 32 only: before others were left out, 24 heads of 80 and 48, chunks of 32, took 94 us by 64 and 73 by 32; longer chunks were not measured.
 constexpr long kWantedTiles = 256;
 template <class T, class F> inline void for_tile(const ChunkView &c, int rows, int columns, F &&fn)
 {

@@ -12,7 +12,7 @@ struct ChunkView {                     // tokens and their chunks
     int n, batch, heads, tokens, chunk, chunks, f, g;
     const int32_t *lengths;
 };
-// A product of rows within chunks: scores, and (P null) the states' sums.
+// Products of rows within chunks.
 template <class T> struct ScoresArgs {
     ChunkView c;
     const T *decay;
