@@ -479,7 +479,8 @@ spin_status spin_linattn_outputs(const spin_linattn *s, int rows, int columns, i
                                  uint64_t *out, spin_stream stream);
 
 /* One token of every sequence b with active[b] > 0 (active NULL: all):   S' = T(CS + 2^f w[1] S + w[0] k (x) v, f + g),   out = T(CO + q . S', f),
- * S' being opened against S_mask; sum CS = w[0] (sum a_k) (x) (sum a_v), sum CO = (sum a_q) . (sum S_mask).  Of the others S' = S and out = 0.  s->tokens and s->chunk are not looked at, s->lengths is `active`, and decay is [heads][2].
+ * S' being opened against S_mask; sum CS = w[0] (sum a_k) (x) (sum a_v), sum CO = (sum a_q) . (sum S_mask).  Of the others S' = S and out = 0.
+ * s->tokens and s->chunk are not looked at, s->lengths is `active`, and decay is [heads][2].
  * q, k: [n][batch][heads][rows]; v, CO, tO, out: [n][batch][heads][columns]; S, S_mask, CS, tS, S_out: [n][batch][heads][rows][columns].  S_out may alias S, S_mask, CS or
  * an array of tS; out CO or an array of tO.                                                                                 */
 spin_status spin_linattn_step(const spin_linattn *s, int rows, int columns, const uint64_t *S, const spin_masked *q, const spin_masked *k,
